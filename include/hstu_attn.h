@@ -361,6 +361,106 @@ int hstu_cp_reorder(int32_t batch, int64_t total_rows, int32_t cp_size, int32_t 
                     const int64_t* row_bytes, int64_t local_rows, const int32_t* seq_offsets,
                     void* hip_stream);
 
+/* ---- rotary positions -----------------------------------------------------------------------
+ * A term of positions inside the scores: before the attention the pairs of elements of q and k rows are
+ * turned by angles proportional to the row's position p,
+ *     y_a = scale * (x_a cos(p f_j) - x_b sin(p f_j)),   y_b = scale * (x_b cos(p f_j) + x_a sin(p f_j)),
+ * so that <q_i, k_j> depends on positions through i - j only.  Pair j of a head, j < rotary_dim / 2, is the elements
+ * (j, j + rotary_dim / 2), or (2 j, 2 j + 1) where `interleaved`; elements from rotary_dim on are copied.  Angles are
+ * worked out in double precision, the turn in fp32, rounded once.  Scaled frequencies (long contexts) are the
+ * caller's: any f_j will do. */
+typedef struct {
+  const double* inv_freq;      /* device, [rotary_dim / 2]: radians per position                          */
+  int32_t rotary_dim;          /* a multiple of 16, 16 .. the head dimension                                */
+  int32_t interleaved;         /* 0: pairs (j, j + rotary_dim / 2), 1: pairs (2 j, 2 j + 1)                  */
+  float scale;                 /* factor of cosines and sines (1, or what a long-context scaling asks for) */
+  int32_t reserved;            /* must be 0 */
+} hstu_rotary_desc;
+
+typedef struct {
+  const void* src;             /* rows of num_heads * head_dim contiguous elements, src_stride apart        */
+  void* dst;                   /* ... dst_stride apart; dst == src (and equal strides): in place            */
+  int64_t src_stride;          /* elements from row to row, >= num_heads * head_dim, whole 16 bytes          */
+  int64_t dst_stride;
+  int32_t num_heads;
+  int32_t head_dim;            /* 32, 64 or 128                                                             */
+} hstu_rotary_tensor;
+
+/* Turns the rows of up to 4 tensors (e.g. q and k, which may have different numbers of heads) in one launch.
+ * positions: int32 [rows], or NULL: a row's place in its sequence, from seq_offsets int32 [batch + 1] (rows outside every sequence
+ * are left alone).  backward = 1 turns by the opposite angles: src are the gradients of the turned rows, dst receives those of
+ * the rows before the turn (the map is linear, so nothing else is needed).  No workspace. */
+int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype, int32_t batch, int64_t rows,
+                int32_t num_tensors, const hstu_rotary_tensor* tensors, const int32_t* positions,
+                const int32_t* seq_offsets, void* hip_stream);
+
+/* ---- serving: a paged cache of keys and values ----------------------------------------------
+ * A model that serves keeps the keys and values of every user's history and computes only new rows.  The cache is cut
+ * into pages of page_size rows; page_table names the pages of each sequence in order, so histories grow without being
+ * moved.  Row p of sequence b is row p % page_size of page page_table[b * table_stride + p / page_size].  Inside a
+ * page each key/value head's rows are contiguous: k_pages [num_pages][num_kv_heads][page_size][d_qk], v_pages the same with
+ * d_v, pages k_page_stride / v_page_stride elements apart (K and V may be halves of one buffer).
+ * seq_lens[b] counts the rows of sequence b INCLUDING the new rows of the call; the m_b = seq_offsets[b + 1] - seq_offsets[b]
+ * new rows are its last ones, at positions seq_lens[b] - m_b .. seq_lens[b] - 1.
+ * Nothing of the cache is read on the host.  Whatever table and lengths hold, nothing outside the pages is touched: lengths
+ * count as at least 0 and at most pages_per_seq * page_size, rows in a page whose id is not in 0 .. num_pages - 1 are dropped by an append and
+ * count as zeros in the attention.  Rows behind a sequence's length and pages that the table does not name may hold anything,
+ * NaN included. */
+typedef struct {
+  int32_t batch;               /* sequences: rows of page_table, entries of seq_lens                       */
+  int32_t num_kv_heads;        /* >= 1                                                                      */
+  int32_t d_qk, d_v;           /* 32, 64 or 128                                                             */
+  int32_t page_size;           /* rows per page: a power of two, 16 .. 32768                                */
+  int32_t pages_per_seq;       /* entries of a row of page_table that may be read, >= 0                      */
+  int32_t dtype;               /* hstu_dtype of the cache and of the call's rows                            */
+  int32_t reserved;            /* must be 0                                                                 */
+  int64_t num_pages;           /* 0 .. 2^31 - 1                                                             */
+  int64_t k_page_stride;       /* elements, >= num_kv_heads * page_size * d_qk, whole 16 bytes              */
+  int64_t v_page_stride;
+  int64_t table_stride;        /* entries from row to row of page_table, >= pages_per_seq                    */
+  void* k_pages;
+  void* v_pages;
+  int32_t* ts_pages;           /* [num_pages][page_size] timestamps of the rows, or NULL (no timestamp bias) */
+  const int32_t* page_table;
+  const int32_t* seq_lens;     /* [batch] */
+} hstu_paged_cache;
+
+/* Writes the new rows of k [new_rows, num_kv_heads, d_qk] and v [new_rows, num_kv_heads, d_v] (rows k_stride / v_stride
+ * elements apart) to their places in the cache, the keys turned by their positions where `rotary` is not NULL.  q, if not
+ * NULL, is turned in the same launch (rows of head_dim d_qk).  timestamps: int32 [new_rows], required iff the cache holds
+ * timestamps.  A row without a place (negative position, no entry or no such page) is dropped.  The pages of the new rows of
+ * different sequences have to be different ones. */
+int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rotary, int64_t new_rows,
+                      const hstu_rotary_tensor* q, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      const int32_t* timestamps, const int32_t* seq_offsets, void* hip_stream);
+
+typedef struct {
+  int32_t num_heads;           /* query heads: a multiple of num_kv_heads; head h reads key/value head
+                                  h / (num_heads / num_kv_heads)                                            */
+  int32_t max_len;             /* N >= 1: the normaliser 1/N                                                */
+  float alpha;                 /* scale inside the SiLU                                                     */
+  int32_t causal;              /* 1: a new row sees the cached rows up to its own position; 0: all of them
+                                  (rows that are not in the cache, scored against it)                       */
+  int32_t out_dtype;           /* the cache's dtype or HSTU_F32                                             */
+  int32_t max_kv;              /* a bound on seq_lens that the caller knows, or 0: only the division of the work
+                                  depends on it, longer sequences are computed all the same                 */
+  int64_t new_rows;            /* rows of q and o, 0 <= new_rows * num_heads / num_kv_heads < 2^31 - 256     */
+} hstu_paged_attn_params;
+
+/* O_i = sum over the visible cached rows j of SiLU(alpha (<q_i, k_j> + bias_ij)) v_j / max_len for the new rows i of every
+ * sequence (o: [new_rows, num_heads, d_v], contiguous; q rows q_stride elements apart).  The cached rows must be there:
+ * append first.  A row that sees nothing gets zeros; rows of o outside every sequence are left alone.  bias: NULL, or the timestamp bias with the
+ * timestamps of the new rows (those of the cached rows are the cache's; d_ts_weights is not used).  The work is divided
+ * by the lengths on the device, long histories among many workgroups, whose partial sums are added in the order of the keys: results
+ * repeat bit for bit, and depend on the batch only in the order of fp32 additions.  bf16: as in hstu_jagged_attn_fwd; a call
+ * of few rows per sequence keeps P in two bf16 terms. */
+int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_cache* cache, const hstu_ts_bias* bias,
+                        const void* q, int64_t q_stride, const int32_t* seq_offsets, void* o, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of workspace of that call (0 on invalid input): depends on the shapes alone, not on pointers. */
+size_t hstu_paged_attn_workspace_bytes(const hstu_paged_attn_params* params, const hstu_paged_cache* cache);
+
 /* Bytes of workspace the given entry point needs for `params` (an upper bound
  * that depends on batch, total_rows, num_heads, d_v and dtype only; 0 on invalid params).
  * Schedules, plus for bf16 forward passes with a forced tile height a transposed copy of V, plus
@@ -412,7 +512,8 @@ int hstu_debug_dump_schedule(const hstu_attn_params* params, const hstu_cp_desc*
  *          8 scaling of the bias table's gradient, 9 matrix-instruction loop, 10 atomic-rate kernel,
  *          11 backward in one launch (short sequences; small fp32 calls), 12 forward and dq pass of a partial in
  *          one kernel, 13 dk/dv pass of a large batch whose workgroups walk over runs of equal work; every other
- *          form of the dk/dv pass is 1) and its duration in milliseconds; returns the number written (<= capacity)
+ *          form of the dk/dv pass is 1; 14 rotary positions, 15 append to a paged cache, 16 attention over a paged cache,
+ *          17 sum of its partial results) and its duration in milliseconds; returns the number written (<= capacity)
  *          or a status < 0.
  */
 int hstu_debug_timing_begin(int max_records);

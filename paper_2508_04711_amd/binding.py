@@ -105,6 +105,39 @@ class _RingDesc(ctypes.Structure):
     ]
 
 
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class _RotaryTensor(ctypes.Structure):
+    _fields_ = [
+        ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_stride", ctypes.c_int64),
+        ("dst_stride", ctypes.c_int64), ("num_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+    ]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("d_qk", ctypes.c_int32), ("d_v", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("pages_per_seq", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32), ("num_pages", ctypes.c_int64), ("k_page_stride", ctypes.c_int64),
+        ("v_page_stride", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p), ("ts_pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("seq_lens", ctypes.c_void_p),
+    ]
+
+
+class _PagedParams(ctypes.Structure):
+    _fields_ = [
+        ("num_heads", ctypes.c_int32), ("max_len", ctypes.c_int32), ("alpha", ctypes.c_float),
+        ("causal", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("max_kv", ctypes.c_int32),
+        ("new_rows", ctypes.c_int64),
+    ]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -172,6 +205,18 @@ def load_library():
     lib.hstu_debug_dq_atomic_rate.restype = ctypes.c_int
     lib.hstu_debug_dq_atomic_rate.argtypes = [vp, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.POINTER(ctypes.c_double), vp]
+    rp, cp = ctypes.POINTER(_RotaryDesc), ctypes.POINTER(_PagedCache)
+    lib.hstu_rotary.restype = ctypes.c_int
+    lib.hstu_rotary.argtypes = [rp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                ctypes.POINTER(_RotaryTensor), vp, i32p, vp]
+    lib.hstu_cache_append.restype = ctypes.c_int
+    lib.hstu_cache_append.argtypes = [cp, rp, ctypes.c_int64, ctypes.POINTER(_RotaryTensor), vp, ctypes.c_int64, vp,
+                                      ctypes.c_int64, vp, i32p, vp]
+    lib.hstu_paged_attn_fwd.restype = ctypes.c_int
+    lib.hstu_paged_attn_fwd.argtypes = [ctypes.POINTER(_PagedParams), cp, bp, vp, ctypes.c_int64, i32p, vp, vp,
+                                        ctypes.c_size_t, vp]
+    lib.hstu_paged_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.hstu_paged_attn_workspace_bytes.argtypes = [ctypes.POINTER(_PagedParams), cp]
     lib.hstu_schedule_tile_rows.restype = ctypes.c_int
     lib.hstu_schedule_tile_rows.argtypes = [pp, ctypes.c_int]
     _lib = lib
@@ -618,7 +663,7 @@ def hstu_debug_dump_schedule(seq_offsets: torch.Tensor, total_rows: int, num_hea
 
 KERNEL_KINDS = {0: "fwd", 1: "dkdv", 2: "dq", 3: "plan", 4: "transpose", 5: "reorder", 6: "reduce",
                 7: "ts_records", 8: "dw_finish", 9: "mfma_loop", 10: "dq_atomic", 11: "bwd", 12: "fwd_dq",
-                13: "dkdv_runs"}
+                13: "dkdv_runs", 14: "rotary", 15: "append", 16: "paged_attn", 17: "paged_reduce"}
 
 
 def hstu_debug_mfma_loop(random_operands: bool, iterations: int, sink: torch.Tensor, stream=None) -> float:
@@ -834,3 +879,311 @@ def hstu_cp_ring_pass_bias(q_local: torch.Tensor, d_o_local: Optional[torch.Tens
                              accumulate_dkv=accumulate_dkv, out=out, recv=recv, workspace=workspace,
                              stream=stream, copy_stream=copy_stream,
                              _bias=(q_timestamps, ts_parts, ts_weights, groups_log2, dw))
+
+
+# ---- rotary positions, the paged cache and the attention over it ------------------------------------------------------
+
+def hstu_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                            trained_len: int = 0, turns_low: float = 1.0, turns_high: float = 32.0,
+                            device=None) -> torch.Tensor:
+    """Radians per position of the rotary_dim / 2 pairs, fp64: f_j = base ** (-2 j / rotary_dim), for contexts `factor`
+    times as long as those trained on scaled by
+
+      "none"      nothing
+      "linear"    all frequencies / factor (positions interpolated)
+      "base"      the base * factor ** (rotary_dim / (rotary_dim - 2)): the lowest frequency / factor, the highest kept
+      "by_parts"  frequencies that turn at least turns_high times over trained_len positions kept, those that turn at most
+                  turns_low times / factor, a linear blend between
+    """
+    if rotary_dim < 16 or rotary_dim % 16 != 0:
+        raise ValueError("rotary_dim must be a positive multiple of 16")
+    if not base > 0 or not factor > 0:
+        raise ValueError("base and factor must be positive")
+    if scaling not in ("none", "linear", "base", "by_parts"):
+        raise ValueError("unknown scaling %r" % (scaling,))
+    if scaling == "base":
+        base = base * factor ** (rotary_dim / (rotary_dim - 2.0))
+    f = np.float64(base) ** (-2.0 * np.arange(rotary_dim // 2, dtype=np.float64) / rotary_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_parts":
+        if trained_len < 1 or not turns_high > turns_low:
+            raise ValueError("by_parts needs trained_len >= 1 and turns_high > turns_low")
+        turns = trained_len * f / (2.0 * np.pi)
+        keep = np.clip((turns - turns_low) / (turns_high - turns_low), 0.0, 1.0)
+        f = f * keep + f / factor * (1.0 - keep)
+    return torch.from_numpy(f).to(torch.device("cuda") if device is None else device)
+
+
+def _check_rows(t: torch.Tensor, name: str, device, dtype=None) -> None:
+    """[rows, heads, dim] of one device whose rows are contiguous (a slice of a wider projection is one)."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError("%s must be a device tensor [rows, heads, dim]" % name)
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if not t.is_contiguous() and ((t.shape[2] > 1 and t.stride(2) != 1)
+                                  or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError("%s: a row's heads must be contiguous" % name)
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    # (the stride of a single row says nothing)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _check_index(t: torch.Tensor, name: str, device, size: Optional[int] = None) -> None:
+    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous() \
+            or (size is not None and t.shape[0] != size):
+        raise ValueError("%s must be a contiguous 1-d int32 tensor on %s%s"
+                         % (name, device, "" if size is None else " with %d entries" % size))
+
+
+def _rotary_desc(inv_freq: torch.Tensor, interleaved: bool, scale: float, device) -> _RotaryDesc:
+    if inv_freq.dtype != torch.float64 or inv_freq.device != device or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous 1-d fp64 tensor on %s (hstu_rotary_frequencies)" % (device,))
+    return _RotaryDesc(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale, 0)
+
+
+def _on_its_device(fn):
+    """Runs `fn` with the device of its first argument (a tensor, a list of them, a cache) as the current one, and its stream=
+    argument as torch's current stream (see _allocates_on_its_stream)."""
+    @functools.wraps(fn)
+    def wrapped(first, *args, **kwargs):
+        t = first[0] if isinstance(first, (list, tuple)) and len(first) else first
+        device = getattr(t, "device", None)
+        if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
+            with torch.cuda.device(device):
+                return wrapped(first, *args, **kwargs)
+        stream = kwargs.get("stream")
+        if stream is None or stream == torch.cuda.current_stream():
+            return fn(first, *args, **kwargs)
+        if device is not None and stream.device != device:
+            raise ValueError("stream is of %s, the tensors are on %s" % (stream.device, device))
+        with torch.cuda.stream(stream):
+            return fn(first, *args, **kwargs)
+    return wrapped
+
+
+def _rotary_call(where, backward, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, stream):
+    tensors = list(tensors)
+    n = len(tensors)
+    if not 1 <= n <= 4:
+        raise ValueError("1 to 4 tensors per call")
+    first = tensors[0]
+    device, rows = first.device, first.shape[0]
+    if out is None:
+        out = [torch.empty(t.shape, dtype=t.dtype, device=device) for t in tensors]
+    elif len(out) != n:
+        raise ValueError("one output per tensor")
+    arr = (_RotaryTensor * n)()
+    for i, (t, o) in enumerate(zip(tensors, out)):
+        _check_rows(t, "tensors[%d]" % i, device, first.dtype)
+        if o is not t:
+            _check_rows(o, "out[%d]" % i, device, first.dtype)
+        if t.shape[0] != rows or o.shape != t.shape:
+            raise ValueError("tensors and outputs must have the same rows, an output its tensor's shape")
+        arr[i] = _RotaryTensor(t.data_ptr(), o.data_ptr(), _row_stride(t), _row_stride(o), t.shape[1], t.shape[2])
+    if (seq_offsets is None) == (positions is None):
+        raise ValueError("either seq_offsets or positions")
+    batch = 0
+    if positions is not None:
+        _check_index(positions, "positions", device, rows)
+    else:
+        _check_index(seq_offsets, "seq_offsets", device)
+        batch = seq_offsets.shape[0] - 1
+    desc = _rotary_desc(inv_freq, interleaved, scale, device)
+    rc = load_library().hstu_rotary(ctypes.byref(desc), backward, _dtype_code(first), batch, rows, n, arr,
+                                    _ptr(positions), _ptr(seq_offsets), _stream(stream))
+    if rc != 0:
+        raise HstuError(rc, where)
+    return out
+
+
+@_on_its_device
+def hstu_rotary_fwd(tensors, inv_freq: torch.Tensor, seq_offsets: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0,
+                    out=None, stream=None):
+    """Turns the rows of 1 to 4 tensors [rows, heads, dim] (q and k, say) by their positions: their places in their sequences
+    (seq_offsets) or `positions` (int32, one per row).
+
+    inv_freq: fp64 [rotary_dim / 2], see hstu_rotary_frequencies; the first rotary_dim elements of every head are turned, as pairs
+    (j, j + rotary_dim / 2) or, interleaved, (2 j, 2 j + 1).  `out` may pass the outputs, the tensors themselves
+    to turn them in place.  Rows may be slices of a wider projection.  Returns the list of outputs.
+    """
+    return _rotary_call("hstu_rotary_fwd", 0, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, stream)
+
+
+@_on_its_device
+def hstu_rotary_bwd(tensors, inv_freq: torch.Tensor, seq_offsets: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0,
+                    out=None, stream=None):
+    """Gradients of the rows before hstu_rotary_fwd (same arguments), given those of the turned rows (dq and dk of
+    hstu_jagged_attn_bwd, say): the turn by the opposite angles."""
+    return _rotary_call("hstu_rotary_bwd", 1, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, stream)
+
+
+class HstuPagedCache:
+    """The buffers of a paged cache of keys and values, checked once (struct hstu_paged_cache of include/hstu_attn.h).
+
+    k_pages [num_pages, kv_heads, page_size, d_qk], v_pages [num_pages, kv_heads, page_size, d_v] (pages may lie apart, as the
+    halves of one buffer [num_pages, 2, ...] do), page_table int32 [batch, pages_per_seq], seq_lens int32
+    [batch]: rows of each sequence in the cache, the new rows of a call included; ts_pages int32 [num_pages, page_size]: the rows'
+    timestamps, for models with the timestamp bias.  The cache is the caller's: table and lengths are read when a call
+    runs, so a program changes them in place (and captured calls see the change).
+    """
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
+                 ts_pages: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 4 or v_pages.dim() != 4 or not k_pages.is_cuda:
+            raise ValueError("k_pages and v_pages must be device tensors [num_pages, kv_heads, page_size, dim]")
+        device, dtype = k_pages.device, k_pages.dtype
+        pages, heads, ps, dqk = k_pages.shape
+        dv = v_pages.shape[3]
+        if v_pages.shape[:3] != k_pages.shape[:3] or v_pages.dtype != dtype or v_pages.device != device:
+            raise ValueError("k_pages and v_pages must have the same pages, heads, page size, dtype and device")
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            if pages > 0 and not t[0].is_contiguous():
+                raise ValueError("%s: a page must be contiguous" % name)
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.device != device or \
+                (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be an int32 tensor [batch, pages_per_seq] on %s, rows contiguous" % (device,))
+        _check_index(seq_lens, "seq_lens", device, page_table.shape[0])
+        if ts_pages is not None and (ts_pages.dtype != torch.int32 or ts_pages.device != device
+                                     or tuple(ts_pages.shape) != (pages, ps) or not ts_pages.is_contiguous()):
+            raise ValueError("ts_pages must be a contiguous int32 tensor [num_pages, page_size] on %s" % (device,))
+        self.k_pages, self.v_pages, self.page_table, self.seq_lens, self.ts_pages = \
+            k_pages, v_pages, page_table, seq_lens, ts_pages
+        self.device, self.dtype = device, dtype
+        self.batch, self.pages_per_seq = page_table.shape
+        self.num_kv_heads, self.page_size, self.d_qk, self.d_v = heads, ps, dqk, dv
+        self._struct = _PagedCache(
+            self.batch, heads, dqk, dv, ps, self.pages_per_seq, _code(dtype), 0, pages,
+            k_pages.stride(0) if pages > 1 else heads * ps * dqk, v_pages.stride(0) if pages > 1 else heads * ps * dv,
+            page_table.stride(0) if self.batch > 1 else self.pages_per_seq, k_pages.data_ptr(), v_pages.data_ptr(),
+            _ptr(ts_pages), page_table.data_ptr(), seq_lens.data_ptr())
+
+
+@_on_its_device
+def hstu_cache_append(cache: HstuPagedCache, k: torch.Tensor, v: torch.Tensor, seq_offsets: torch.Tensor,
+                      q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                      interleaved: bool = False, scale: float = 1.0, timestamps: Optional[torch.Tensor] = None,
+                      q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Writes the new rows k [rows, kv_heads, d_qk], v [rows, kv_heads, d_v] (sequence b's: seq_offsets[b] ..
+    seq_offsets[b + 1] - 1) into the cache as the last rows of their sequences (cache.seq_lens counts them already).
+
+    inv_freq (and interleaved, scale; see hstu_rotary_fwd) turns k, and q if it is given, by the rows' positions on the way;
+    returns the turned q (q_out, which may be q itself, or a new tensor), None without q.  timestamps: int32 [rows], needed
+    iff the cache holds timestamps.
+    """
+    device, dtype = cache.device, cache.dtype
+    rows = k.shape[0]
+    _check_rows(k, "k", device, dtype)
+    _check_rows(v, "v", device, dtype)
+    if k.shape[1:] != (cache.num_kv_heads, cache.d_qk) or v.shape != (rows, cache.num_kv_heads, cache.d_v):
+        raise ValueError("k and v must be [rows, %d, %d] and [rows, %d, %d]"
+                         % (cache.num_kv_heads, cache.d_qk, cache.num_kv_heads, cache.d_v))
+    _check_index(seq_offsets, "seq_offsets", device, cache.batch + 1)
+    if (timestamps is None) != (cache.ts_pages is None):
+        raise ValueError("timestamps are needed iff the cache holds timestamps")
+    if timestamps is not None:
+        _check_index(timestamps, "timestamps", device, rows)
+    desc = None if inv_freq is None else ctypes.byref(_rotary_desc(inv_freq, interleaved, scale, device))
+    tensor = None
+    if q is not None:
+        _check_rows(q, "q", device, dtype)
+        if q.shape[0] != rows or q.shape[2] != cache.d_qk:
+            raise ValueError("q must be [%d, heads, %d]" % (rows, cache.d_qk))
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=device)
+        else:
+            _check_rows(q_out, "q_out", device, dtype)
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+        tensor = ctypes.byref(_RotaryTensor(q.data_ptr(), q_out.data_ptr(), _row_stride(q), _row_stride(q_out),
+                                            q.shape[1], q.shape[2]))
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rc = load_library().hstu_cache_append(ctypes.byref(cache._struct), desc, rows, tensor, k.data_ptr(), _row_stride(k),
+                                          v.data_ptr(), _row_stride(v), _ptr(timestamps), seq_offsets.data_ptr(),
+                                          _stream(stream))
+    if rc != 0:
+        raise HstuError(rc, "hstu_cache_append")
+    return q_out
+
+
+def _paged_params(heads, max_len, alpha, causal, out_dtype, max_kv, rows) -> _PagedParams:
+    return _PagedParams(heads, max_len, alpha, 1 if causal else 0, _code(out_dtype), 0 if max_kv is None else max_kv, rows)
+
+
+def hstu_paged_attn_workspace_bytes(cache: HstuPagedCache, num_heads: int, new_rows: int,
+                                    max_kv: Optional[int] = None) -> int:
+    """Bytes of workspace of an attention call of `new_rows` rows over the cache (0: out of range)."""
+    p = _paged_params(num_heads, 1, 1.0, True, cache.dtype, max_kv, new_rows)
+    return int(load_library().hstu_paged_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(cache._struct)))
+
+
+def _paged_call(where, q, cache, seq_offsets, bias, max_len, alpha, causal, max_kv, out, workspace, stream, out_dtype):
+    device = cache.device
+    _check_rows(q, "q", device, cache.dtype)
+    rows, heads, dim = q.shape
+    if dim != cache.d_qk or heads % cache.num_kv_heads != 0:
+        raise ValueError("q must be [rows, a multiple of %d heads, %d]" % (cache.num_kv_heads, cache.d_qk))
+    _check_index(seq_offsets, "seq_offsets", device, cache.batch + 1)
+    if out is None:
+        odt = cache.dtype if out_dtype is None else out_dtype
+        if dim == cache.d_v and odt is cache.dtype:
+            out = _empty(q, odt)
+        else:
+            out = torch.empty((rows, heads, cache.d_v), dtype=odt, device=device)
+    else:
+        odt = out.dtype
+        _check_tensor(out, "out", rows, heads, cache.d_v, odt)
+        if out.device != device or (out_dtype is not None and out_dtype != odt):
+            raise ValueError("out must be %s on %s" % (out_dtype or odt, device))
+    lib = load_library()
+    p = ctypes.byref(_paged_params(heads, max_len, alpha, causal, odt, max_kv, rows))
+    c = ctypes.byref(cache._struct)
+    if workspace is None:
+        workspace = torch.empty(max(lib.hstu_paged_attn_workspace_bytes(p, c), 256), dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on %s" % (device,))
+    rc = lib.hstu_paged_attn_fwd(p, c, bias, q.data_ptr(), _row_stride(q), seq_offsets.data_ptr(), out.data_ptr(),
+                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc != 0:
+        raise HstuError(rc, where)
+    return out
+
+
+@_on_its_device
+def hstu_paged_attn_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: torch.Tensor, max_len: int, alpha: float,
+                        causal: bool = True, max_kv: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None,
+                        out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """Attention of new rows q [rows, heads, d_qk] over the cached rows of their sequences: [rows, heads, d_v].
+
+    causal: the new rows are the last seq_offsets[b + 1] - seq_offsets[b] rows of the cache (append them first) and see the rows up to
+    their own; otherwise every row sees all cached rows of its sequence (candidates scored against a history).
+    heads may be a multiple of the cache's.  max_kv: a bound on cache.seq_lens that the caller knows (a hint for the
+    division of the work; nothing is left out beyond it).
+    """
+    return _paged_call("hstu_paged_attn_fwd", q, cache, seq_offsets, None, max_len, alpha, causal, max_kv, out, workspace,
+                       stream, out_dtype)
+
+
+@_on_its_device
+def hstu_paged_attn_bias_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: torch.Tensor, timestamps: torch.Tensor,
+                             ts_weights: torch.Tensor, groups_log2: int, max_len: int, alpha: float, causal: bool = True,
+                             max_kv: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None, stream=None,
+                             out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """hstu_paged_attn_fwd with the timestamp bias of hstu_jagged_attn_bias_fwd: timestamps [rows] of the new rows against
+    the cached rows' (cache.ts_pages)."""
+    if cache.ts_pages is None:
+        raise ValueError("the cache holds no timestamps")
+    if q.device != cache.device or timestamps.device != cache.device or ts_weights.device != cache.device:
+        raise ValueError("q, timestamps and ts_weights must be on %s" % (cache.device,))
+    bias = _bias_desc(timestamps, ts_weights, None, groups_log2, q.shape[0])
+    return _paged_call("hstu_paged_attn_bias_fwd", q, cache, seq_offsets, ctypes.byref(bias), max_len, alpha, causal, max_kv,
+                       out, workspace, stream, out_dtype)

@@ -4,45 +4,20 @@
 #include <cmath>
 #include <cstdlib>
 #include <mutex>
-#include <vector>
 
 #include "../../include/hstu_attn.h"
 #include "hstu_common.h"
+#include "hstu_timing.h"
+
+namespace hstu {
+thread_local Timing g_timing;
+}
 
 namespace {
 
 using namespace hstu;
 
 bool dim_ok(int d) { return d == 32 || d == 64 || d == 128; }
-
-// Optional per-launch timing (hstu_debug_timing_begin/end): thread-local, off by default.
-struct Timing {
-  bool on = false;
-  std::vector<hipEvent_t> start, stop;
-  std::vector<int> kind;
-  size_t used = 0;
-};
-thread_local Timing g_timing;
-
-struct TimedLaunch {
-  hipStream_t stream;
-  bool active;
-  TimedLaunch(int kind, hipStream_t s) : stream(s), active(false) {
-    Timing& t = g_timing;
-    if (t.on && t.used < t.start.size()) {
-      active = true;
-      t.kind[t.used] = kind;
-      (void)hipEventRecord(t.start[t.used], stream);
-    }
-  }
-  ~TimedLaunch() {
-    if (active) {
-      Timing& t = g_timing;
-      (void)hipEventRecord(t.stop[t.used], stream);
-      ++t.used;
-    }
-  }
-};
 
 int check_params(const hstu_attn_params* p) {
   if (!p) return HSTU_ERR_NULL_PTR;

@@ -1,0 +1,289 @@
+// What the kernels of the paged cache share (not part of the C ABI): the view of a cache, and the schedule of the attention of
+// new rows over it.
+#pragma once
+#include "hstu_common.h"
+
+namespace hstu {
+
+// A paged cache on the device.  Page p holds, per key/value head, `ps` rows: [heads][ps][d].
+struct PagedView {
+  const char* k;              // pages of K and V
+  const char* v;
+  int64_t k_page, v_page;     // bytes from page to page
+  const int32_t* table;       // [batch][table_stride] page ids
+  int64_t table_stride;
+  const int32_t* lens;        // [batch] rows in the cache, the new ones among them
+  int32_t* ts;                // [num_pages][ps] timestamps, or null
+  uint32_t num_pages;
+  int32_t ps_log2;            // page size 16 << n
+  int32_t cap;                // rows a sequence's part of the table has room for
+};
+
+struct PagedArgs {
+  PagedView c;
+  const char* q;              // [rows][heads][d_qk], rows q_stride bytes apart
+  int64_t q_stride;
+  const int32_t* off;         // [batch + 1] offsets of the new rows
+  const int32_t* ts_q;        // timestamps of the new rows; ts_w: the bias table (nb entries, 2^f groups an octave)
+  const float* ts_w;
+  int32_t nb, f;
+  void* o;                    // [rows][heads][d_v]
+  float* partial;             // two slots per worker
+  int32_t batch, rows, heads, kv_heads, group;
+  int32_t causal, out_f32;
+  float alpha, inv_n;
+  int32_t workers;            // a multiple of 8
+  int32_t whole;              // every worker takes one tile, uncut
+  int32_t min_share;          // keys a worker takes at least
+};
+
+// The schedule.  For one key/value head of one sequence the (new row, query head) pairs that read it are numbered
+// row * group + head and cut into tiles of QT pairs; a tile streams over the keys that its last row sees.  What a tile costs is
+// counted in keys times `group` (so that the causal sum over tiles has a closed form), TILE_KEYS for its own loads and stores
+// included.  The tiles of all sequences and heads in order form one line, of which every worker takes an equal length
+// (min_share at least): no sequence however long or short leaves a worker idle, and nothing is read on the host.  A worker that
+// starts or ends inside a tile writes an fp32 partial result; SiLU attention is a plain sum over keys, so joining the parts is
+// an addition (reduce kernel, in the order of the keys: results repeat bit for bit).
+constexpr int TILE_KEYS = 32;
+
+struct SeqWork {
+  int m, n;      // new rows, cached rows
+  int row0;      // first new row
+  int tiles;     // of one head
+  int64_t base;  // cost of tile t is base + (causal ? (t + 1) * QT : 0)
+  int64_t cost;  // of one head
+};
+
+__device__ __forceinline__ int64_t tiles_cost(const SeqWork& s, int64_t t, int qt, bool causal) {
+  return t * s.base + (causal ? qt * (t * (t + 1) / 2) : 0);
+}
+
+template <int QT>
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int b) {
+  SeqWork s;
+  int e;
+  seq_range(a.off, b, a.rows, s.row0, e);
+  s.m = e - s.row0;
+  s.n = clampi(a.c.lens[b], 0, a.c.cap);
+  s.tiles = (int)(((int64_t)s.m * a.group + QT - 1) / QT);
+  if (a.whole) {
+    s.base = 1;
+    s.cost = s.tiles;
+  } else {
+    const int keys = a.causal ? (s.n > s.m ? s.n - s.m : 0) : s.n;
+    s.base = (int64_t)(keys + TILE_KEYS) * a.group;
+    s.cost = tiles_cost(s, s.tiles, QT, a.causal != 0);
+  }
+  return s;
+}
+
+// Place of cost unit x: sequence, head, tile, and the unit's place inside the tile.
+struct Place {
+  int b, h, t;
+  int64_t u;     // place inside the tile
+  SeqWork s;
+};
+
+// Inclusive prefix sums of 64-bit values over the wave.
+__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)x >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int l) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, l);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), l);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// The line of all work, seen by one wave: lane i sums the sequences [i * chunk, (i + 1) * chunk).
+template <int QT>
+struct Line {
+  int chunk;
+  int64_t incl, sum;  // of the lane's sequences and all before them; of the lane's alone
+  int64_t total;
+
+  __device__ __forceinline__ void init(const PagedArgs& a) {
+    const int lane = threadIdx.x & 63;
+    chunk = (a.batch + 63) >> 6;
+    sum = 0;
+    const int64_t b0 = (int64_t)lane * chunk;
+    for (int i = 0; i < chunk; ++i)
+      if (b0 + i < a.batch) sum += seq_work<QT>(a, (int)b0 + i).cost;
+    sum *= a.kv_heads;
+    incl = wave_scan64(sum);
+    total = lane64(incl, 63);
+  }
+
+  // (x < total)
+  __device__ __forceinline__ Place find(const PagedArgs& a, int64_t x) const {
+    const int lane = threadIdx.x & 63;
+    const uint64_t past = __ballot(incl <= x);
+    const int l = __popcll(past);  // first lane whose sum reaches beyond x
+    int64_t before = lane64(incl - sum, l);
+    int b = l * chunk;
+    for (int left = chunk; chunk > 1 && left > 0; left -= 64) {  // sequences b .. b + 63 of the lane's, one per lane
+      int64_t c = 0;
+      if (lane < left && b + lane < a.batch) c = seq_work<QT>(a, b + lane).cost * a.kv_heads;
+      const int64_t in = wave_scan64(c);
+      const uint64_t p = __ballot(before + in <= x);
+      const int j = __popcll(p);
+      if (j < 64) {
+        before += lane64(in - c, j);
+        b += j;
+        break;
+      }
+      before += lane64(in, 63);
+      b += 64;
+    }
+    Place r;
+    r.b = __builtin_amdgcn_readfirstlane(b);
+    r.s = seq_work<QT>(a, r.b);
+    const int64_t rel = uniform64(x - before);
+    r.h = 0;
+    r.t = 0;
+    int64_t y = rel;
+    if (a.kv_heads > 1) {
+      r.h = (int)(y / r.s.cost);
+      y -= (int64_t)r.h * r.s.cost;
+    }
+    if (r.s.tiles > 1) {
+      const bool causal = a.causal && !a.whole;
+      if (!causal) {
+        r.t = (int)(y / r.s.base);
+      } else {
+        int lo = 0, hi = r.s.tiles;  // tiles_cost(lo) <= y < tiles_cost(hi)
+        while (hi - lo > 1) {
+          const int mid = lo + (hi - lo) / 2;
+          if (tiles_cost(r.s, mid, QT, true) <= y) lo = mid; else hi = mid;
+        }
+        r.t = lo;
+      }
+      y -= tiles_cost(r.s, r.t, QT, causal);
+    }
+    r.u = y;
+    return r;
+  }
+};
+
+// The length of the line a worker takes, and the workers that get any.
+__device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t total) {
+  if (a.whole) return 1;
+  const int64_t s = (total + a.workers - 1) / a.workers, least = (int64_t)a.min_share * a.group;
+  return s > least ? s : least;
+}
+
+// Workers in the order of the line: consecutive ones, which may share keys (tiles of one head, one range), are put on one XCD.
+// Workgroups are dealt to the 8 XCDs in turn.
+__device__ __forceinline__ int64_t worker_place(int w, int64_t active) {
+  const int64_t per = (active + 7) >> 3;
+  return w < 8 * per ? (int64_t)(w & 7) * per + (w >> 3) : active;
+}
+
+// One tile's part [u0, u1) of its cost, as keys [k0, k1).
+struct Segment {
+  int64_t u0, u1, cost;
+  int k0, k1;    // keys of this part
+  int lim0;      // keys the tile's first row sees
+  int vis;       // keys its last row sees
+  int pairs;     // pairs in the tile
+  bool first, last;  // the part holds the tile's first / last keys
+};
+
+template <int QT>
+__device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWork& s, int t, int64_t u0, int64_t room) {
+  Segment g;
+  const bool causal = a.causal && !a.whole;
+  g.cost = s.base + (causal ? (int64_t)(t + 1) * QT : 0);
+  g.u0 = u0;
+  g.u1 = g.cost - u0 < room ? g.cost : u0 + room;
+  g.first = u0 == 0;
+  g.last = g.u1 == g.cost;
+  const int64_t all = (int64_t)s.m * a.group, p0 = (int64_t)t * QT;
+  g.pairs = all - p0 < QT ? (int)(all - p0) : QT;
+  g.vis = s.n;
+  g.lim0 = s.n;
+  if (a.causal) {
+    const int row0 = (int)(p0 / a.group), row1 = (int)((p0 + g.pairs - 1) / a.group);
+    g.lim0 = clampi((int64_t)s.n - s.m + row0 + 1, 0, s.n);
+    g.vis = clampi((int64_t)s.n - s.m + row1 + 1, 0, s.n);
+  }
+  // (cuts lie at multiples of 32 keys; the part after a cut works the same key out)
+  auto key = [&](int64_t u) {
+    const int64_t k = (u / a.group - TILE_KEYS) & ~(int64_t)31;
+    return clampi(k, 0, g.vis);
+  };
+  g.k0 = g.first ? 0 : key(g.u0);
+  g.k1 = g.last ? g.vis : key(g.u1);
+  return g;
+}
+
+// Moves on to the next tile of the line.
+template <int QT>
+__device__ __forceinline__ void next_tile(const PagedArgs& a, Place& p) {
+  p.u = 0;
+  if (++p.t < p.s.tiles) return;
+  p.t = 0;
+  if (++p.h < a.kv_heads) return;
+  p.h = 0;
+  do {
+    if (++p.b >= a.batch) return;
+    p.s = seq_work<QT>(a, p.b);
+  } while (p.s.cost == 0);
+}
+
+// Page ids of a sequence, 64 at a time in the lanes of a register: ids outside the cache become -1 (such a page's rows count as
+// zeros: nothing is read through a wrong id), and so do entries behind the last one that is needed.
+struct PageIds {
+  int first, ids;  // ids: lane i holds entry first + i
+  __device__ __forceinline__ void fill(const PagedView& c, int b, int entry, int entries) {
+    first = entry;
+    const int i = entry + (int)(threadIdx.x & 63);
+    int id = -1;
+    if (i < entries) id = c.table[(int64_t)b * c.table_stride + i];
+    ids = (uint32_t)id < c.num_pages ? id : -1;
+  }
+  __device__ __forceinline__ int get(int entry) const { return __builtin_amdgcn_readlane(ids, entry - first); }
+  __device__ __forceinline__ bool holds(int entry) const { return (uint32_t)(entry - first) < 64u; }
+};
+
+// pairs of (q row, head) per tile and one-wave workers
+constexpr int FEW_PAIRS = 16;
+constexpr int MANY_PAIRS = 128;
+hipError_t launch_paged_few(const PagedArgs& a, int dtype_f32, int d_qk, int d_v, hipStream_t stream);
+hipError_t launch_paged_many(const PagedArgs& a, int d_qk, int d_v, hipStream_t stream);
+// Adds up the partial results of cut tiles.  many: of the kernel with tiles of MANY_PAIRS.
+hipError_t launch_paged_reduce(const PagedArgs& a, int many, int d_v, hipStream_t stream);
+
+// Rotation and appending.
+struct RotaryTensor {
+  const char* src;
+  char* dst;
+  int64_t src_stride, dst_stride;  // bytes from row to row (dst: from page to page where `paged`)
+  int32_t heads, d, rotate, paged;
+};
+struct RotaryArgs {
+  RotaryTensor t[4];
+  int32_t count;
+  const double* freq;    // radians per position, rotary / 2 of them
+  int32_t rotary, interleaved;
+  float scale, sign;     // sign: +1 forward, -1 backward
+  const int32_t* pos;    // positions of the rows, or null: places in their sequences
+  const int32_t* off;
+  int32_t batch, rows;
+  PagedView c;           // appending
+  const int32_t* ts;     // timestamps of the rows, or null
+};
+hipError_t launch_rotary(const RotaryArgs& a, int dtype_f32, hipStream_t stream);
+hipError_t launch_append(const RotaryArgs& a, int dtype_f32, hipStream_t stream);
+
+}  // namespace hstu

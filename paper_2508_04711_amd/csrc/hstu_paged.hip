@@ -1,0 +1,562 @@
+// Attention of few new rows over a paged cache (the next event of each user, a handful of them), and the sum of the parts of
+// cut tiles.
+//
+//   O_i = (1 / N) sum over the visible cached rows j of silu(alpha (q_i . k_j [+ w(i, j)])) v_j
+//
+// One new row reads every cached key and value of its sequence once and does 4 d flops per row of 4 d bytes (bf16): the pass is
+// bound by reading the cache, and everything here serves to keep loads in flight.
+//   - A wave is a worker of its own (no LDS, no barrier): it takes a run of the line of all work (hstu_paged.h) and streams
+//     blocks of keys through registers, the next block's loads issued before the present one is used; with two waves
+//     per SIMD that is up to 256 KB in flight per CU, four times what the memory's latency needs.
+//   - 16 (new row, query head) pairs that share a key/value head are one operand of the 16x16 matrix instructions: query heads
+//     that share keys, and a few new rows, cost no further reads.  One pair alone leaves 15 columns unused: the matrix pipe
+//     then still has 5 times the throughput that the loads can feed.
+//   - S^T = K Q^T leaves P^T in the accumulators as the second product's operand (its contraction index is
+//     matched to them by the choice of the rows a lane loads), and V's rows are loaded whole, 16 bytes per lane, and transposed
+//     inside the lane (one byte permutation per register): nothing goes through LDS.
+//   - P enters the second product as two bf16 terms, whose sum is exact to 2^-17 of it, for 8 more matrix instructions per block
+//     in a loop that waits for memory: the result is off by its own rounding alone.
+//   - Rows behind the part's end and rows of pages that do not exist lie outside the buffer descriptors: they arrive as zeros
+//     without traffic, so what such memory holds (other users' rows, NaN) has no way in.
+#include "hstu_mfma.h"
+#include "hstu_paged.h"
+
+namespace hstu {
+
+namespace {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+// Descriptor of `rows` rows (of `row_bytes`) from p on; loads beyond them return zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* p, int rows, int row_bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows * row_bytes, 0x00020000);
+}
+
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&dst)[W], __amdgpu_buffer_rsrc_t r, int voff, int soff) {
+  if constexpr (W == 4) {
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = x[i];
+  } else if constexpr (W == 2) {
+    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, 0);
+    dst[0] = x[0]; dst[1] = x[1];
+  } else {
+    dst[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, soff, 0);
+  }
+}
+
+// What a block of a tile's stream needs besides its own keys.
+struct TileCtx {
+  int lim;       // keys the lane's pair sees
+  int lim0, vis; // ... the tile's first and last row see
+  int tq;        // the lane's pair's timestamp
+  float c1;      // -alpha log2 e
+  const float* wtab;
+  int nb, f;
+};
+
+// Where 16 rows of one page are: keys [key, key + 16) of a sequence, for one head.
+struct Rows16 {
+  const char* k;
+  const char* v;
+  const int32_t* ts;
+  int n;         // rows of them that belong to the part (0: none, or no such page)
+};
+template <int ROW_K, int ROW_V>
+__device__ __forceinline__ Rows16 rows16(const PagedView& c, const PageIds& ids, int h, int key, int end) {
+  const int id = ids.get(key >> c.ps_log2);
+  const int slot = key & ((1 << c.ps_log2) - 1);
+  Rows16 r;
+  const int64_t row = ((int64_t)h << c.ps_log2) + slot, page = id < 0 ? 0 : id;
+  r.k = c.k + page * c.k_page + row * ROW_K;
+  r.v = c.v + page * c.v_page + row * ROW_V;
+  r.ts = c.ts + (page << c.ps_log2) + slot;
+  const int left = end - key;
+  r.n = id < 0 || left < 0 ? 0 : (left < 16 ? left : 16);
+  return r;
+}
+
+// ---- bf16 ----------------------------------------------------------------------------------------------------------------
+//   v_mfma_f32_16x16x32_bf16  D[16x16] += A[16x32] B[32x16]   (lane l: i = l % 16, g = l / 16)
+//     A: lane holds row i, k = 8 g .. 8 g + 7     B: column i, same k     D: column i, rows 4 g + r, r = 0..3
+// Block of 32 keys: two S^T products (keys 0..15 and 16..31 as rows), whose accumulators hold for the lane's pair the keys
+// 4 g + r and 16 + 4 g + r; those eight are the contraction index 8 g .. 8 g + 7 of the second product, so lane (i, g) loads
+// these eight rows of V, at elements VE * i .. of each (VE = d_v / 16), and product e of VE makes the output's elements VE * row + e.
+template <int DQK, int DV, bool BIAS>
+struct FewBf16 {
+  static constexpr int BK = 32, PARTS = 2, KS = DQK / 32, VE = DV / 16, VW = VE / 2;
+  static constexpr int ROW_K = DQK * 2, ROW_V = DV * 2;
+  struct Block {
+    uint32_t k[2][KS][4];
+    uint32_t v[8][VW];
+    uint32_t ts[2][4];
+  };
+  Block b;
+  bf16x8 q[KS];
+  f32x4 acc[VE];
+  int ko, vo, to;  // the lane's byte offsets inside 16 rows
+
+  __device__ __forceinline__ void init() {
+    const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    ko = i * ROW_K + g * 16;
+    vo = 4 * g * ROW_V + i * VE * 2;
+    to = 16 * g;
+  }
+  __device__ __forceinline__ void start(const char* qrow) {  // qrow: the lane's pair's row, or null
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 z = {0, 0, 0, 0};
+      if (qrow) z = *(const u32x4*)(qrow + ks * 64 + g * 16);
+      q[ks] = __builtin_bit_cast(bf16x8, z);
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void where(Rows16 (&r)[PARTS], const PagedView& c, const PageIds& ids, int h, int key, int end) const {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) r[x] = rows16<ROW_K, ROW_V>(c, ids, h, key + 16 * x, end);
+  }
+  __device__ __forceinline__ void fetch_k(const Rows16 (&r)[PARTS]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const __amdgpu_buffer_rsrc_t rk = rows_rsrc(r[x].k, r[x].n, ROW_K);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) load_words<4>(b.k[x][ks], rk, ko + ks * 64, 0);
+      if constexpr (BIAS) load_words<4>(b.ts[x], rows_rsrc((const char*)r[x].ts, r[x].n, 4), to, 0);
+    }
+  }
+  __device__ __forceinline__ void fetch_v(const Rows16 (&r)[PARTS]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const __amdgpu_buffer_rsrc_t rv = rows_rsrc(r[x].v, r[x].n, ROW_V);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) load_words<VW>(b.v[4 * x + e], rv, vo + e * ROW_V, 0);
+    }
+  }
+  // V's operand of output elements VE * row + e, rows behind `lim` of the block's keys left out where CUT.
+  template <bool CUT>
+  __device__ __forceinline__ bf16x8 v_operand(int e, int lim, int g) const {
+    u32x4 w;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      uint32_t lo = b.v[2 * p][e >> 1], hi = b.v[2 * p + 1][e >> 1];
+      if constexpr (CUT) {
+        const int key = (p >> 1) * 16 + 4 * g + 2 * (p & 1);
+        lo = key < lim ? lo : 0;
+        hi = key + 1 < lim ? hi : 0;
+      }
+      w[p] = __builtin_amdgcn_perm(hi, lo, (e & 1) ? 0x07060302 : 0x05040100);
+    }
+    return __builtin_bit_cast(bf16x8, w);
+  }
+  float p[8];
+  __device__ __forceinline__ void scores(const TileCtx& t) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (BIAS)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = t.wtab[bias_bucket(abs_diff(t.tq, (int)b.ts[x][r]), t.nb, t.f)];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 z = {b.k[x][ks][0], b.k[x][ks][1], b.k[x][ks][2], b.k[x][ks][3]};
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, z), q[ks], s, 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[4 * x + r] = s[r];
+    }
+  }
+  __device__ __forceinline__ void values(const TileCtx& t, int key) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] *= sigmoid_scaled(p[e], t.c1);
+    const bool masked = t.lim0 < t.vis && key + BK > t.lim0;
+    if (masked) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = key + (e >> 2) * 16 + 4 * g + (e & 3) < t.lim ? p[e] : 0.f;
+    }
+    bf16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      hi[e] = (__bf16)p[e];
+      lo[e] = (__bf16)(p[e] - (float)hi[e]);
+    }
+    if (masked) {
+      // Rows of V that some pairs see and others do not: an infinity or NaN there times a zero of P would reach the pairs that
+      // do not see it, so such a block is multiplied once per row position, without the rows behind it.
+      uint32_t bad = 0;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          const uint32_t w = b.v[r][i];
+          bad |= (uint32_t)((w & 0x7f80u) == 0x7f80u) | (uint32_t)((w & 0x7f800000u) == 0x7f800000u);
+        }
+      if (__ballot(bad != 0) != 0) {
+        for (int lim = t.lim0; lim <= t.vis; ++lim) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const bf16x8 v = v_operand<true>(e, lim - key, g);
+            f32x4 part = acc[e];
+            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, part, 0, 0, 0);
+            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, part, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[e][r] = t.lim == lim ? part[r] : acc[e][r];
+          }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const bf16x8 v = v_operand<false>(e, 0, g);
+      acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, acc[e], 0, 0, 0);
+      acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, acc[e], 0, 0, 0);
+    }
+  }
+  // The lane's part of its pair's output row: elements 4 VE g .. + 4 VE - 1.
+  __device__ __forceinline__ void result(float (&x)[4 * VE]) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) x[r * VE + e] = acc[e][r];
+  }
+  static constexpr int OUT = 4 * VE;
+};
+
+// ---- fp32 ----------------------------------------------------------------------------------------------------------------
+//   v_mfma_f32_16x16x4_f32  D[16x16] += A[16x4] B[4x16]: A lane holds row i, k = g; B column i, same k; D as above.
+// Block of 16 keys.  The contraction over d_qk takes element 16 s + 4 g + e of a row at step (s, e); the one over keys takes key
+// 4 g + r at step r, which is what accumulator register r holds; lane (i, g) loads V's rows 4 g + r at elements
+// 16 VE j + VE i .. (VE = min(4, d_v / 16)), and product (j, e) makes the output's elements 16 VE j + VE * row + e.
+template <int DQK, int DV, bool BIAS>
+struct FewF32 {
+  static constexpr int BK = 16, PARTS = 1, KS = DQK / 16, VE = DV >= 64 ? 4 : 2, NJ = DV / (16 * VE);
+  static constexpr int ROW_K = DQK * 4, ROW_V = DV * 4;
+  struct Block {
+    uint32_t k[KS][4];
+    uint32_t v[4][NJ][VE];
+    uint32_t ts[4];
+  };
+  Block b;
+  float q[KS][4];
+  f32x4 acc[NJ][VE];
+  int ko, vo, to;
+
+  __device__ __forceinline__ void init() {
+    const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    ko = i * ROW_K + g * 16;
+    vo = 4 * g * ROW_V + i * VE * 4;
+    to = 16 * g;
+  }
+  __device__ __forceinline__ void start(const char* qrow) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (qrow) z = *(const float4*)(qrow + s * 64 + g * 16);
+      q[s][0] = z.x; q[s][1] = z.y; q[s][2] = z.z; q[s][3] = z.w;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) acc[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void where(Rows16 (&r)[PARTS], const PagedView& c, const PageIds& ids, int h, int key, int end) const {
+    r[0] = rows16<ROW_K, ROW_V>(c, ids, h, key, end);
+  }
+  __device__ __forceinline__ void fetch_k(const Rows16 (&r)[PARTS]) {
+    const __amdgpu_buffer_rsrc_t rk = rows_rsrc(r[0].k, r[0].n, ROW_K);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) load_words<4>(b.k[s], rk, ko + s * 64, 0);
+    if constexpr (BIAS) load_words<4>(b.ts, rows_rsrc((const char*)r[0].ts, r[0].n, 4), to, 0);
+  }
+  __device__ __forceinline__ void fetch_v(const Rows16 (&r)[PARTS]) {
+    const __amdgpu_buffer_rsrc_t rv = rows_rsrc(r[0].v, r[0].n, ROW_V);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) load_words<VE>(b.v[e][j], rv, vo + e * ROW_V + j * 16 * VE * 4, 0);
+  }
+  f32x4 s;
+  __device__ __forceinline__ void scores(const TileCtx& t) {
+    s = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (BIAS)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[r] = t.wtab[bias_bucket(abs_diff(t.tq, (int)b.ts[r]), t.nb, t.f)];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, b.k[ks][e]), q[ks][e], s, 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(const TileCtx& t, int key) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = s[r] * sigmoid_scaled(s[r], t.c1);
+    const bool masked = t.lim0 < t.vis && key + BK > t.lim0;
+    if (masked) {
+      asm volatile("" ::: "memory");
+      uint32_t bad = 0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[r] = key + 4 * g + r < t.lim ? p[r] : 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) bad |= (uint32_t)((b.v[r][j][e] & 0x7f800000u) == 0x7f800000u);
+      }
+      if (__ballot(bad != 0) != 0) {  // (as in bf16)
+        for (int lim = t.lim0; lim <= t.vis; ++lim)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              f32x4 part = acc[j][e];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float v = key + 4 * g + r < lim ? __builtin_bit_cast(float, b.v[r][j][e]) : 0.f;
+                part = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[r], part, 0, 0, 0);
+              }
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[j][e][r] = t.lim == lim ? part[r] : acc[j][e][r];
+            }
+        return;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+          acc[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, b.v[r][j][e]), p[r], acc[j][e], 0, 0, 0);
+  }
+  __device__ __forceinline__ void result(float (&x)[4 * VE * NJ]) const {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[(j * 4 + r) * VE + e] = acc[j][e][r];
+  }
+  static constexpr int OUT = 4 * VE * NJ;
+};
+
+template <bool F32, int DQK, int DV, bool BIAS>
+using Few = typename std::conditional<F32, FewF32<DQK, DV, BIAS>, FewBf16<DQK, DV, BIAS>>::type;
+
+// Element of the output row that the lane's value x of result() is.
+template <bool F32, int DV>
+__device__ __forceinline__ int out_element(int x, int g) {
+  if constexpr (!F32) {
+    return (DV / 4) * g + x;
+  } else {
+    constexpr int VE = DV >= 64 ? 4 : 2;
+    const int j = x / (4 * VE), y = x % (4 * VE);
+    return 16 * VE * j + 4 * VE * g + y;
+  }
+}
+
+template <bool F32, int DQK, int DV, bool BIAS>
+__global__ void __launch_bounds__(64, 2) paged_few_kernel(PagedArgs a) {
+  typedef Few<F32, DQK, DV, BIAS> F;
+  constexpr int BK = F::BK, ES = F32 ? 4 : 2;
+  __shared__ float wtab[BIAS ? MAX_TS_BUCKETS : 1];
+  const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
+
+  Line<FEW_PAIRS> line;
+  line.init(a);
+  if (line.total == 0) return;
+  const int64_t share = share_of(a, line.total), active = (line.total + share - 1) / share;
+  const int64_t w = worker_place(blockIdx.x, active);
+  if (w >= active) return;
+  if constexpr (BIAS) {
+    for (int x = lane; x < a.nb; x += 64) wtab[x] = a.ts_w[x];
+    __syncthreads();
+  }
+  int64_t at = w * share;
+  const int64_t end = at + share < line.total ? at + share : line.total;
+  Place pl = line.find(a, at);
+
+  F f;
+  f.init();
+  TileCtx t;
+  t.c1 = -a.alpha * 1.4426950408889634f;
+  t.wtab = wtab;
+  t.nb = a.nb;
+  t.f = a.f;
+  t.tq = 0;
+  while (at < end && pl.b < a.batch) {
+    const Segment sg = make_segment<FEW_PAIRS>(a, pl.s, pl.t, pl.u, end - at);
+    // the lane's pair
+    const int pair = pl.t * FEW_PAIRS + i;
+    const int row = pair / a.group, head = pl.h * a.group + pair % a.group;
+    const bool on = i < sg.pairs;
+    const int64_t qrow = pl.s.row0 + row;
+    if constexpr (BIAS) t.tq = on ? a.ts_q[qrow] : 0;
+    t.lim0 = sg.lim0;
+    t.vis = sg.vis;
+    t.lim = a.causal ? clampi((int64_t)pl.s.n - pl.s.m + row + 1, 0, pl.s.n) : pl.s.n;
+    f.start(on ? a.q + qrow * a.q_stride + (int64_t)head * DQK * ES : nullptr);
+
+    if (sg.k0 < sg.k1) {
+      PageIds ids;
+      const int entries = (sg.k1 + (1 << a.c.ps_log2) - 1) >> a.c.ps_log2;
+      ids.fill(a.c, pl.b, sg.k0 >> a.c.ps_log2, entries);
+      Rows16 r[F::PARTS];
+      auto where = [&](int key) {  // (behind the part's end: rows of no length, so that every path issues the same loads)
+        const bool more = key < sg.k1;
+        if (more && !ids.holds((key + BK - 1) >> a.c.ps_log2)) ids.fill(a.c, pl.b, key >> a.c.ps_log2, entries);
+        f.where(r, a.c, ids, pl.h, more ? key : sg.k0, more ? sg.k1 : sg.k0);
+      };
+      where(sg.k0);
+      f.fetch_k(r);
+      f.fetch_v(r);
+      for (int key = sg.k0; key < sg.k1; key += BK) {
+        f.scores(t);
+        __builtin_amdgcn_sched_barrier(0);
+        where(key + BK);
+        f.fetch_k(r);
+        __builtin_amdgcn_sched_barrier(0);
+        f.values(t, key);
+        __builtin_amdgcn_sched_barrier(0);
+        f.fetch_v(r);
+      }
+    }
+
+    if (on) {
+      float x[F::OUT];
+      f.result(x);
+      if (sg.first && sg.last) {
+        const float scale = a.alpha * a.inv_n;
+        const int64_t elem = (qrow * a.heads + head) * DV;
+        if (a.out_f32) {
+#pragma unroll
+          for (int y = 0; y < F::OUT; y += 4)
+            *(float4*)((float*)a.o + elem + out_element<F32, DV>(y, g)) =
+                make_float4(x[y] * scale, x[y + 1] * scale, x[y + 2] * scale, x[y + 3] * scale);
+        } else {
+#pragma unroll
+          for (int y = 0; y < F::OUT; y += 4) {
+            bf16x4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = (__bf16)(x[y + e] * scale);
+            *(bf16x4*)((__bf16*)a.o + elem + out_element<F32, DV>(y, g)) = z;
+          }
+        }
+      } else {
+        float* slot = a.partial + ((2 * w + (sg.first ? 1 : 0)) * FEW_PAIRS + i) * DV;
+#pragma unroll
+        for (int y = 0; y < F::OUT; y += 4)
+          *(float4*)(slot + out_element<F32, DV>(y, g)) = make_float4(x[y], x[y + 1], x[y + 2], x[y + 3]);
+      }
+    }
+    at += sg.u1 - sg.u0;
+    next_tile<FEW_PAIRS>(a, pl);
+  }
+}
+
+// ---- sum of the parts ------------------------------------------------------------------------------------------------------
+// Workgroup w finds the tile that worker w began and did not finish (if there is one: workers work the same line out), and
+// adds up its parts: slot 2 w + 1, then slot 2 x of the workers x = w + 1, ... whose run the tile reaches into.
+constexpr int REDUCE_THREADS = 256;
+template <int QT, int DV>
+__global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs a) {
+  constexpr int RW = DV / 4;  // float4 of a row
+  __shared__ float4 sums[REDUCE_THREADS];
+  Line<QT> line;
+  line.init(a);
+  if (line.total == 0) return;
+  const int64_t share = share_of(a, line.total), active = (line.total + share - 1) / share;
+  const int64_t w = blockIdx.x;
+  const int64_t end = (w + 1) * share;
+  if (w >= active || end >= line.total) return;  // (the line's end is a tile's end)
+  // the tile that holds the run's last unit
+  const Place pl = line.find(a, end - 1);
+  const Segment sg = make_segment<QT>(a, pl.s, pl.t, pl.u, 1);
+  const int64_t tile0 = end - 1 - pl.u, tile1 = tile0 + sg.cost;
+  if (tile0 < w * share || tile1 <= end) return;  // begun before, or finished
+  const int parts = (int)((tile1 - 1) / share - w) + 1;
+
+  // threads: RW per row; rows and, where rows are few, runs of parts
+  const int cols = sg.pairs * RW;
+  const int groups = cols >= REDUCE_THREADS ? 1 : REDUCE_THREADS / cols;
+  const int per = (parts + groups - 1) / groups;
+  const float scale = a.alpha * a.inv_n;
+  for (int c0 = 0; c0 < cols; c0 += REDUCE_THREADS) {
+    const int tid = threadIdx.x, grp = groups > 1 ? tid / cols : 0, c = groups > 1 ? tid % cols : c0 + tid;
+    const bool on = grp < groups && c < cols;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (on) {
+      const int x1 = (grp + 1) * per < parts ? (grp + 1) * per : parts;
+#pragma unroll 4
+      for (int x = grp * per; x < x1; ++x) {
+        const int64_t slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
+        const float4 y = *(const float4*)(a.partial + slot * QT * DV + (int64_t)c * 4);
+        s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+      }
+    }
+    if (groups > 1) {
+      sums[tid] = s;
+      __syncthreads();
+      if (grp == 0 && on)
+        for (int x = 1; x < groups; ++x) {
+          const float4 y = sums[x * cols + c];
+          s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+        }
+    }
+    if (on && grp == 0) {
+      const int pair = pl.t * QT + c / RW, row = pair / a.group, head = pl.h * a.group + pair % a.group;
+      const int64_t elem = ((int64_t)(pl.s.row0 + row) * a.heads + head) * DV + (c % RW) * 4;
+      if (a.out_f32) {
+        *(float4*)((float*)a.o + elem) = make_float4(s.x * scale, s.y * scale, s.z * scale, s.w * scale);
+      } else {
+        bf16x4 z;
+        z[0] = (__bf16)(s.x * scale); z[1] = (__bf16)(s.y * scale); z[2] = (__bf16)(s.z * scale); z[3] = (__bf16)(s.w * scale);
+        *(bf16x4*)((__bf16*)a.o + elem) = z;
+      }
+    }
+  }
+}
+
+template <bool F32, int DQK, int DV>
+hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
+  if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true>), dim3((unsigned)a.workers), dim3(64), 0, stream, a);
+  else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false>), dim3((unsigned)a.workers), dim3(64), 0, stream, a);
+  return hipGetLastError();
+}
+template <bool F32, int DQK>
+hipError_t launch_few_dv(const PagedArgs& a, int d_v, hipStream_t stream) {
+  return d_v == 32 ? launch_few<F32, DQK, 32>(a, stream)
+                   : (d_v == 64 ? launch_few<F32, DQK, 64>(a, stream) : launch_few<F32, DQK, 128>(a, stream));
+}
+template <bool F32>
+hipError_t launch_few_d(const PagedArgs& a, int d_qk, int d_v, hipStream_t stream) {
+  return d_qk == 32 ? launch_few_dv<F32, 32>(a, d_v, stream)
+                    : (d_qk == 64 ? launch_few_dv<F32, 64>(a, d_v, stream) : launch_few_dv<F32, 128>(a, d_v, stream));
+}
+template <int QT>
+hipError_t launch_reduce(const PagedArgs& a, int d_v, hipStream_t stream) {
+  const dim3 grid((unsigned)a.workers), block(REDUCE_THREADS);
+  if (d_v == 32) hipLaunchKernelGGL((paged_reduce_kernel<QT, 32>), grid, block, 0, stream, a);
+  else if (d_v == 64) hipLaunchKernelGGL((paged_reduce_kernel<QT, 64>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((paged_reduce_kernel<QT, 128>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_few(const PagedArgs& a, int dtype_f32, int d_qk, int d_v, hipStream_t stream) {
+  return dtype_f32 ? launch_few_d<true>(a, d_qk, d_v, stream) : launch_few_d<false>(a, d_qk, d_v, stream);
+}
+
+hipError_t launch_paged_reduce(const PagedArgs& a, int many, int d_v, hipStream_t stream) {
+  return many ? launch_reduce<MANY_PAIRS>(a, d_v, stream) : launch_reduce<FEW_PAIRS>(a, d_v, stream);
+}
+
+}  // namespace hstu

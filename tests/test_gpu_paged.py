@@ -1,0 +1,390 @@
+"""Appending to a paged cache and the attention of new rows over it, against the definitions in float64 (oracle/serve.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_04711_amd as hstu
+from oracle import serve
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+NAN = float("nan")
+
+
+def _f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+class Problem:
+    """A cache with histories of `lens` rows (the last `new` of them new), pages in random order, and what no sequence owns
+    filled with NaN: behind the histories, in free pages, in table entries behind the last."""
+
+    def __init__(self, dtype, lens, new, heads=2, kv_heads=2, dqk=64, dv=64, ps=16, seed=0, spare=3, fill=NAN, buckets=0, std=0.7):
+        rng = np.random.default_rng(seed)
+        g = torch.Generator().manual_seed(seed)
+        self.dtype, self.lens, self.new, self.ps, self.buckets = dtype, list(lens), list(new), ps, buckets
+        need = [-(-n // ps) for n in lens]
+        self.pages = sum(need) + spare
+        self.width = max(need + [1]) + 1
+        order = rng.permutation(self.pages)
+        table = rng.integers(0, self.pages, size=(len(lens), self.width)).astype(np.int32)
+        at = 0
+        kp = torch.full((self.pages, kv_heads, ps, dqk), fill)
+        vp = torch.full((self.pages, kv_heads, ps, dv), fill)
+        tp = torch.from_numpy(rng.integers(-2 ** 31, 2 ** 31, size=(self.pages, ps)).astype(np.int32))
+        for b, n in enumerate(lens):
+            table[b, :need[b]] = order[at:at + need[b]]
+            at += need[b]
+            stamps = np.sort(rng.integers(0, 2 ** 22, size=n)).astype(np.int32)
+            for p in range(0, n, ps):
+                pg, m = table[b, p // ps], min(ps, n - p)
+                kp[pg, :, :m] = torch.randn((kv_heads, m, dqk), generator=g) * std
+                vp[pg, :, :m] = torch.randn((kv_heads, m, dv), generator=g) * std
+                tp[pg, :m] = torch.from_numpy(stamps[p:p + m])
+        self.off = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.rows = int(self.off[-1])
+        self.table = table
+        self.q = (torch.randn((self.rows, heads, dqk), generator=g) * std).to(DT[dtype])
+        self.kp, self.vp, self.tp = kp.to(DT[dtype]), vp.to(DT[dtype]), tp
+        self.ts = torch.from_numpy(rng.integers(0, 2 ** 22, size=self.rows).astype(np.int32))
+        self.w = torch.randn(max(buckets, 1), generator=g)
+        self.alpha, self.max_len = dqk ** -0.5, max(self.lens + [1])
+
+    def cache(self):
+        return hstu.HstuPagedCache(self.kp.cuda(), self.vp.cuda(), torch.from_numpy(self.table).cuda(),
+                                   torch.tensor(self.lens, dtype=torch.int32).cuda(),
+                                   self.tp.cuda() if self.buckets else None)
+
+    def call(self, cache=None, q=None, **kw):
+        cache = self.cache() if cache is None else cache
+        q = self.q.cuda() if q is None else q
+        off = torch.from_numpy(self.off).cuda()
+        causal = kw.pop("causal", True)
+        if self.buckets:
+            return hstu.hstu_paged_attn_bias_fwd(q, cache, off, self.ts.cuda(), self.w.cuda(), 2, self.max_len, self.alpha,
+                                                 causal, **kw)
+        return hstu.hstu_paged_attn_fwd(q, cache, off, self.max_len, self.alpha, causal, **kw)
+
+    def want(self, causal=True):
+        bias = dict(ts=self.ts.numpy(), ts_pages=self.tp.numpy(), weights=self.w.numpy().astype(np.float64), f=2) if self.buckets else {}
+        return serve.attention(_f64(self.q), _f64(self.kp), _f64(self.vp), self.table, self.lens, self.off, self.max_len,
+                               self.alpha, causal, **bias)
+
+    def check(self, got, causal=True, out_dtype=None, one_term=None):
+        o, sums = self.want(causal)
+        bf16 = self.dtype == "bf16"
+        one_term = bf16 if one_term is None else one_term  # (calls of many rows keep P in one bf16 term)
+        tol = serve.attention_tolerance(o, sums, self.q.shape[2], max(self.lens + [1]), bf16, got.dtype == torch.bfloat16, one_term)
+        g = _f64(got)
+        assert g.shape == o.shape
+        assert np.isfinite(g).all()
+        err = np.abs(g - o)
+        assert (err <= tol).all(), float((err / tol).max())
+
+
+LENS = [
+    ([1], [1]), ([200], [1]), ([17, 0, 1, 16, 15, 33, 300], [1] * 7), ([40, 64, 9], [3, 0, 9]), ([0, 0, 5], [0, 2, 7]),
+    ([100, 31, 257], [20, 31, 64]), ([700, 20], [1, 18]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dqk,dv", [(32, 32), (64, 128), (128, 64), (128, 128), (128, 32), (32, 128), (64, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention(dtype, dqk, dv, causal):
+    for i, (lens, new) in enumerate(LENS):
+        if causal:
+            pr = Problem(dtype, lens, new, 2, 2, dqk, dv, 16 << (i % 3), seed=i)
+        else:  # rows that are not in the cache: any number against any history
+            pr = Problem(dtype, lens, new[::-1], 4, 2, dqk, dv, 16 << (i % 3), seed=i)
+        pr.check(pr.call(causal=causal), causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads", [(8, 1), (6, 2), (40, 2), (3, 3)])
+@pytest.mark.parametrize("ps", [16, 64, 256])
+def test_shared_heads_and_page_sizes(dtype, heads, kv_heads, ps):
+    pr = Problem(dtype, [90, 333, 0, 16], [1, 5, 0, 2], heads, kv_heads, 64, 32, ps, seed=ps)
+    for causal in (True, False):
+        pr.check(pr.call(causal=causal), causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dqk,dv", [(128, 128), (32, 64), (64, 32)])
+def test_bias(dtype, dqk, dv):
+    for lens, new, buckets in (([300, 1, 50], [1, 1, 4], 64), ([65, 130], [40, 7], 512), ([400], [70], 1)):
+        pr = Problem(dtype, lens, new, 4, 2, dqk, dv, 16, seed=buckets, buckets=buckets)
+        for causal in (True, False):
+            pr.check(pr.call(causal=causal), causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_output_types_strides_and_outputs(dtype):
+    pr = Problem(dtype, [70, 400], [2, 3], 4, 4, 64, 64, 32)
+    cache = pr.cache()
+    got = pr.call(cache, out_dtype=torch.float32)
+    assert got.dtype == torch.float32
+    pr.check(got)
+    # q as a slice of a fused projection
+    fused = torch.full((pr.rows, 3, 4, 64), NAN, dtype=DT[dtype], device="cuda")
+    fused[:, 1] = pr.q.cuda()
+    out = torch.empty((pr.rows, 4, 64), dtype=torch.float32, device="cuda")
+    assert pr.call(cache, fused[:, 1], out=out) is out
+    assert torch.equal(out, got)
+    # K and V as halves of one buffer, the table as a slice of a wider one
+    both = torch.stack((pr.kp, pr.vp), dim=1).cuda()
+    wide = torch.full((2, 50), -5, dtype=torch.int32, device="cuda")
+    wide[:, :pr.width] = torch.from_numpy(pr.table).cuda()
+    other = hstu.HstuPagedCache(both[:, 0], both[:, 1], wide[:, :pr.width], cache.seq_lens)
+    assert torch.equal(pr.call(other, out_dtype=torch.float32), got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_histories_are_cut_and_joined(dtype):
+    """Few rows over long histories: many workers per tile; a bound on the lengths changes the division alone."""
+    pr = Problem(dtype, [5000, 3, 1777, 0, 2048], [1, 1, 2, 1, 1], 2, 1, 64, 64, 64, seed=5)
+    got = pr.call()
+    pr.check(got)
+    assert torch.equal(got, pr.call())              # the same call, the same bits
+    pr.check(pr.call(max_kv=5000))
+    pr.check(pr.call(max_kv=100))                   # a wrong bound: one worker per tile, nothing left out
+    ws = torch.empty(hstu.hstu_paged_attn_workspace_bytes(pr.cache(), 2, pr.rows), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xff)                                  # (NaN in every partial result: nothing unwritten is read)
+    assert torch.equal(pr.call(workspace=ws), got)
+    with pytest.raises(hstu.HstuError) as e:
+        pr.call(workspace=ws[:1024])
+    assert e.value.status == -4
+
+
+def test_large_batches():
+    """Batches beyond one and beyond 64 sequences per lane of the schedule's scan."""
+    rng = np.random.default_rng(0)
+    for batch, most in ((65, 200), (700, 70), (5000, 20)):
+        lens = rng.integers(0, most, size=batch)
+        new = np.minimum(rng.integers(0, 3, size=batch), lens)
+        pr = Problem("bf16", [int(x) for x in lens], [int(x) for x in new], 1, 1, 32, 32, 16, seed=batch)
+        got = pr.call()
+        pr.check(got)
+        pr.check(pr.call(max_kv=10))
+
+
+def test_rows_outside_stay():
+    pr = Problem("bf16", [30, 50], [2, 3], 2, 2, 64, 64, 16)
+    cache, q = pr.cache(), torch.cat((pr.q, torch.full((4, 2, 64), NAN, dtype=torch.bfloat16))).cuda()
+    out = torch.full((pr.rows + 4, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    hstu.hstu_paged_attn_fwd(q, cache, torch.from_numpy(pr.off).cuda(), pr.max_len, pr.alpha, out=out)
+    pr.check(out[:pr.rows])
+    assert (out[pr.rows:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_that_do_not_exist(dtype):
+    """Wrong ids count as rows of zeros, lengths end at the table's room."""
+    pr = Problem(dtype, [100, 300, 40], [1, 2, 1], 2, 2, 64, 64, 32, fill=0.0)
+    pr.table[0, 1] = -1
+    pr.table[1, 3] = 1 << 30
+    pr.table[2, :] = pr.pages
+    pr.check(pr.call())
+    pr.lens[1] = 10 ** 9   # (rows behind the last page: as many as the table has room for)
+    pr.lens[0] = -5
+    pr.check(pr.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [5, 40])
+def test_nan_in_rows_that_are_not_seen(dtype, new):
+    """Infinities and NaN in new rows reach the rows that see them, and no others."""
+    pr = Problem(dtype, [90], [new], 1, 1, 64, 64, 16)
+    clean, bad = pr.call().float().cpu(), 90 - new + 2      # the third new row's key and value
+    pg, sl = pr.table[0, bad // 16], bad % 16
+    for target, value in ((pr.vp, float("inf")), (pr.kp, NAN)):
+        saved = target[pg, 0, sl, 3].clone()
+        target[pg, 0, sl, 3] = value
+        got = pr.call().float().cpu()
+        assert torch.equal(got[:2], clean[:2])
+        if target is pr.vp:
+            assert not torch.isfinite(got[2:, 0, 3]).any()
+            keep = [i for i in range(64) if i != 3]
+            tol = 2 * serve.UB16 * clean[2:, :, keep].abs() + 1e-6   # (another order of the same sums, rounded to bf16)
+            assert ((got[2:, :, keep] - clean[2:, :, keep]).abs() <= tol).all()
+        else:
+            assert torch.isnan(got[2:]).all()
+        target[pg, 0, sl, 3] = saved
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("inter,rotary", [(False, 64), (True, 32), (False, 0)])
+def test_append(dtype, inter, rotary):
+    lens, new = [40, 0, 17, 5, 100], [3, 0, 17, 9, 70]      # (the fourth: more new rows than its length: some have no place)
+    pr = Problem(dtype, lens, new, 4, 2, 64, 32, 16, fill=1.0, buckets=8)
+    pr.table[4, 2] = -1                                      # a page that does not exist: its rows are dropped
+    cache, off = pr.cache(), torch.from_numpy(pr.off).cuda()
+    g = torch.Generator().manual_seed(3)
+    fused = torch.randn((pr.rows, 2 * 64 + 2 * 32), generator=g).to(DT[dtype]).cuda()
+    k, v = fused[:, :128].view(pr.rows, 2, 64), fused[:, 128:].view(pr.rows, 2, 32)
+    freq = hstu.hstu_rotary_frequencies(rotary) if rotary else None
+    f = freq.cpu().numpy() if rotary else None
+    q = pr.q.cuda()
+    kb, vb, tb = cache.k_pages.clone(), cache.v_pages.clone(), cache.ts_pages.clone()
+    got = hstu.hstu_cache_append(cache, k, v, off, q=q, inv_freq=freq, interleaved=inter, scale=0.9, timestamps=pr.ts.cuda())
+    _, pos = serve.positions(pr.off, pr.rows, lens)
+    seq, _ = serve.positions(pr.off, pr.rows)
+    scale = 0.9
+    for x, y in ((pr.q, got), ):
+        want = serve.rotate(_f64(x), pos, f, inter, scale)
+        tol = serve.rotation_tolerance(_f64(x), want, rotary, inter, scale, dtype == "bf16") if rotary else 0.0
+        assert (np.abs(_f64(y) - want) <= tol).all()
+    kw = serve.rotate(_f64(k), pos, f, inter, scale)
+    tol = serve.rotation_tolerance(_f64(k), kw, rotary, inter, scale, dtype == "bf16") if rotary else np.zeros_like(kw)
+    written = np.zeros((pr.pages, 16), dtype=bool)
+    for r in range(pr.rows):
+        at = serve.place(pr.table, pr.pages, 16, seq[r], int(pos[r]))
+        if at is None:
+            continue
+        pg, sl = at
+        written[pg, sl] = True
+        assert (np.abs(_f64(cache.k_pages[pg, :, sl]) - kw[r]) <= tol[r]).all()
+        assert torch.equal(cache.v_pages[pg, :, sl], v[r])
+        assert int(cache.ts_pages[pg, sl]) == int(pr.ts[r])
+    assert 0 < written.sum() < pr.rows
+    rest = torch.from_numpy(~written).cuda()
+    for before, after in ((kb, cache.k_pages), (vb, cache.v_pages)):
+        assert torch.equal(before.permute(0, 2, 1, 3)[rest], after.permute(0, 2, 1, 3)[rest])
+    assert torch.equal(tb[rest], cache.ts_pages[rest])
+    # q in place, without timestamps in the cache, and without q
+    other = hstu.HstuPagedCache(kb, vb, cache.page_table, cache.seq_lens)
+    assert hstu.hstu_cache_append(other, k, v, off, q=q, q_out=q, inv_freq=freq, interleaved=inter, scale=scale) is q
+    assert torch.equal(q, got) and torch.equal(kb, cache.k_pages) and torch.equal(vb, cache.v_pages)
+    assert hstu.hstu_cache_append(other, k, v, off, inv_freq=freq, interleaved=inter, scale=scale) is None
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_history_served_in_steps_is_the_jagged_attention(dtype, bias):
+    """Positions, append and attention together, as a server runs them: histories arrive in steps (whole chunks, single events,
+    nothing for some users), and every step's outputs are the rows of the training path's forward over the whole
+    histories."""
+    final, heads, d, ps = [150, 37, 201], 2, 64, 16
+    steps = [[100, 0, 180], [49, 36, 1], [0, 0, 19], [1, 1, 1]]
+    g = torch.Generator().manual_seed(1)
+    off = np.concatenate([[0], np.cumsum(final)]).astype(np.int32)
+    rows = int(off[-1])
+    q, k, v = (torch.randn((rows, heads, d), generator=g).mul(0.5).to(DT[dtype]).cuda() for _ in range(3))
+    rng = np.random.default_rng(0)
+    ts = torch.from_numpy(np.concatenate([np.sort(rng.integers(0, 2 ** 20, size=n)) for n in final]).astype(np.int32)).cuda()
+    w = torch.randn(32, generator=g).cuda()
+    doff, freq = torch.from_numpy(off).cuda(), hstu.hstu_rotary_frequencies(d)
+    qr, kr = hstu.hstu_rotary_fwd([q, k], freq, seq_offsets=doff)
+    n, alpha = max(final), d ** -0.5
+    whole = hstu.hstu_jagged_attn_bias_fwd(qr, kr, v, doff, ts, w, 2, n, alpha, True, out_dtype=torch.float32) if bias \
+        else hstu.hstu_jagged_attn_fwd(qr, kr, v, doff, n, alpha, True, out_dtype=torch.float32)
+    pages = sum(-(-x // ps) for x in final) + 1
+    table = torch.from_numpy(rng.permutation(pages)[:3 * 13 if pages >= 39 else pages].astype(np.int32))
+    tab = torch.full((3, 13), -1, dtype=torch.int32)
+    at = 0
+    for b, x in enumerate(final):
+        c = -(-x // ps)
+        tab[b, :c] = table[at:at + c]
+        at += c
+    lens = torch.zeros(3, dtype=torch.int32, device="cuda")
+    cache = hstu.HstuPagedCache(torch.full((pages, heads, ps, d), NAN, dtype=DT[dtype], device="cuda"),
+                                torch.full((pages, heads, ps, d), NAN, dtype=DT[dtype], device="cuda"), tab.cuda(), lens,
+                                torch.zeros((pages, ps), dtype=torch.int32, device="cuda") if bias else None)
+    # both sides keep P in at most one bf16 term and sum in fp32: sums of |p||v| from the oracle bound their difference
+    fq, fk, fv = _f64(qr), _f64(kr), _f64(v)
+    done = [0, 0, 0]
+    for step in steps:
+        pick = np.concatenate([np.arange(off[b] + done[b], off[b] + done[b] + m) for b, m in enumerate(step)]).astype(np.int64)
+        idx = torch.from_numpy(pick).cuda()
+        new = torch.tensor(np.concatenate([[0], np.cumsum(step)]).astype(np.int32)).cuda()
+        lens += torch.tensor(step, dtype=torch.int32, device="cuda")
+        stamps = ts[idx] if bias else None
+        qn = hstu.hstu_cache_append(cache, k[idx], v[idx], new, q=q[idx], inv_freq=freq, timestamps=stamps)
+        assert torch.equal(qn, qr[idx])
+        o = hstu.hstu_paged_attn_bias_fwd(qn, cache, new, stamps, w, 2, n, alpha, out_dtype=torch.float32) if bias \
+            else hstu.hstu_paged_attn_fwd(qn, cache, new, n, alpha, out_dtype=torch.float32)
+        got, want = _f64(o), _f64(whole[idx])
+        for r, row in enumerate(pick):
+            b = int(np.searchsorted(off, row, side="right")) - 1
+            seen = slice(int(off[b]), int(row) + 1)
+            for h in range(heads):
+                x = alpha * (np.abs(fk[seen, h]) @ np.abs(fq[row, h]) + (np.abs(w.cpu().numpy()).max() if bias else 0.0))
+                bound = x @ np.abs(fv[seen, h]) / n     # (|silu(x)| <= |x|)
+                unit = (serve.UB16 if dtype == "bf16" else 0.0) + 400 * serve.U32
+                assert (np.abs(got[r, h] - want[r, h]) <= 2 * unit * bound + 1e-7).all()
+        done = [a + m for a, m in zip(done, step)]
+
+
+def test_two_streams_at_once():
+    """Two calls at the same time, each with its own workspace."""
+    prs = [Problem("bf16", [3000, 100], [1, 1], 4, 4, 128, 128, 64, seed=s, fill=0.0) for s in (1, 2)]
+    caches = [p.cache() for p in prs]
+    want = [p.call(c) for p, c in zip(prs, caches)]
+    qs = [p.q.cuda() for p in prs]
+    off = torch.from_numpy(prs[0].off).cuda()
+    streams = [torch.cuda.Stream() for _ in prs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            got[i].append(hstu.hstu_paged_attn_fwd(qs[i], caches[i], off, prs[i].max_len, prs[i].alpha, stream=s))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w, x) for x in g)
+
+
+def test_captured_step():
+    """Append and attention captured once, replayed while lengths and contents change, with eager work in between."""
+    pr = Problem("bf16", [200, 700, 33], [1, 1, 1], 4, 2, 64, 64, 64, fill=0.0)
+    cache, off = pr.cache(), torch.from_numpy(pr.off).cuda()
+    freq = hstu.hstu_rotary_frequencies(64)
+    q, k, v = pr.q.cuda(), torch.randn((3, 2, 64), device="cuda").bfloat16(), torch.randn((3, 2, 64), device="cuda").bfloat16()
+    qt, out = torch.empty_like(q), torch.empty_like(q)
+    ws = torch.empty(hstu.hstu_paged_attn_workspace_bytes(cache, 4, 3), dtype=torch.uint8, device="cuda")
+
+    def step():
+        hstu.hstu_cache_append(cache, k, v, off, q=q, q_out=qt, inv_freq=freq)
+        hstu.hstu_paged_attn_fwd(qt, cache, off, pr.max_len, pr.alpha, out=out, workspace=ws)
+    step()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for i in range(4):
+        cache.seq_lens.copy_(torch.tensor([200 + i, 700 - 3 * i, 33 + 5 * i], dtype=torch.int32))
+        for t in (q, k, v):
+            t.normal_()
+        out.fill_(NAN)
+        g.replay()
+        torch.cuda.synchronize()
+        got, pages = out.clone(), cache.k_pages.clone()
+        ws.fill_(0xff)
+        step()
+        assert torch.equal(out, got) and torch.equal(cache.k_pages, pages)
+
+
+def test_refusals():
+    pr = Problem("bf16", [30], [2], 2, 2, 64, 64, 16, fill=0.0)
+    cache, off, q = pr.cache(), torch.from_numpy(pr.off).cuda(), pr.q.cuda()
+    call = lambda q=q, off=off, **kw: hstu.hstu_paged_attn_fwd(q, cache, off, 30, 0.1, **kw)
+    for bad in (dict(q=q.float()), dict(q=q[:, :, :32]), dict(q=q[:, :1]), dict(q=q.cpu()), dict(off=off.long()),
+                dict(off=off[:1]), dict(out=q[:1]), dict(out=q, out_dtype=torch.float32), dict(q=q.transpose(0, 1))):
+        with pytest.raises(ValueError):
+            call(**bad)
+    with pytest.raises(ValueError):
+        hstu.hstu_paged_attn_bias_fwd(q, cache, off, pr.ts.cuda(), pr.w.cuda(), 2, 30, 0.1)   # no timestamps in the cache
+    with pytest.raises(ValueError):
+        hstu.hstu_cache_append(cache, q, q, off, timestamps=pr.ts.cuda())
+    with pytest.raises(ValueError):
+        hstu.hstu_cache_append(cache, q[:, :1], q, off)
+    with pytest.raises(ValueError):
+        hstu.hstu_cache_append(cache, q, q, off, q_out=q)
+    kp, vp, tab, lens = cache.k_pages, cache.v_pages, cache.page_table, cache.seq_lens
+    for args in ((kp, vp[:1], tab, lens), (kp, vp.float(), tab, lens), (kp, vp, tab.long(), lens), (kp, vp, tab, lens[:0]),
+                 (kp.transpose(1, 2), vp, tab, lens), (kp, vp, tab.cpu(), lens), (kp, vp, tab, lens, tab)):
+        with pytest.raises(ValueError):
+            hstu.HstuPagedCache(*args)
+    small = hstu.HstuPagedCache(kp[:, :, :8].contiguous(), vp[:, :, :8].contiguous(), tab, lens)
+    with pytest.raises(hstu.HstuError) as e:
+        hstu.hstu_paged_attn_fwd(q, small, off, 30, 0.1)
+    assert e.value.status == -3
