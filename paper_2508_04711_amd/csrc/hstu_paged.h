@@ -19,6 +19,7 @@ struct PagedView {
   int32_t cap;                // rows a sequence's part of the table has room for
 };
 
+struct CutTile;
 struct PagedArgs {
   PagedView c;
   const char* q;              // [rows][heads][d_qk], rows q_stride bytes apart
@@ -28,12 +29,13 @@ struct PagedArgs {
   const float* ts_w;
   int32_t nb, f;
   void* o;                    // [rows][heads][d_v]
+  CutTile* cut;               // one per worker
   float* partial;             // two slots per worker
   int32_t batch, rows, heads, kv_heads, group;
   int32_t causal, out_f32;
   float alpha, inv_n;
   int32_t workers;            // a multiple of 8
-  int32_t whole;              // every worker takes one tile, uncut
+  int32_t whole;              // 1: every worker takes one tile, uncut; 2: ... and is a team of waves
   int32_t min_share;          // keys a worker takes at least
 };
 
@@ -59,22 +61,25 @@ __device__ __forceinline__ int64_t tiles_cost(const SeqWork& s, int64_t t, int q
 }
 
 template <int QT>
-__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int b) {
+__device__ __forceinline__ SeqWork seq_work(const PagedArgs& a, int m, int n, int row0) {
   SeqWork s;
-  int e;
-  seq_range(a.off, b, a.rows, s.row0, e);
-  s.m = e - s.row0;
-  s.n = clampi(a.c.lens[b], 0, a.c.cap);
-  s.tiles = (int)(((int64_t)s.m * a.group + QT - 1) / QT);
+  s.m = m; s.n = n; s.row0 = row0;
+  s.tiles = (int)(((int64_t)m * a.group + QT - 1) / QT);
   if (a.whole) {
     s.base = 1;
     s.cost = s.tiles;
   } else {
-    const int keys = a.causal ? (s.n > s.m ? s.n - s.m : 0) : s.n;
+    const int keys = a.causal ? (n > m ? n - m : 0) : n;
     s.base = (int64_t)(keys + TILE_KEYS) * a.group;
     s.cost = tiles_cost(s, s.tiles, QT, a.causal != 0);
   }
   return s;
+}
+template <int QT>
+__device__ __forceinline__ SeqWork read_work(const PagedArgs& a, int b) {
+  int r, e;
+  seq_range(a.off, b, a.rows, r, e);
+  return seq_work<QT>(a, e - r, clampi(a.c.lens[b], 0, a.c.cap), r);
 }
 
 // Place of cost unit x: sequence, head, tile, and the unit's place inside the tile.
@@ -84,25 +89,32 @@ struct Place {
   SeqWork s;
 };
 
-// Inclusive prefix sums of 64-bit values over the wave.
-__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
+__device__ __forceinline__ int64_t join64(uint32_t lo, uint32_t hi) { return (int64_t)(((uint64_t)hi << 32) | lo); }
 __device__ __forceinline__ int64_t uniform64(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)x >> 32));
-  return (int64_t)(((uint64_t)hi << 32) | lo);
+  return join64(__builtin_amdgcn_readfirstlane((int)(uint32_t)x), __builtin_amdgcn_readfirstlane((int)(x >> 32)));
 }
 __device__ __forceinline__ int64_t lane64(int64_t x, int l) {
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, l);
-  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), l);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
+  return join64(__builtin_amdgcn_readlane((int)(uint32_t)x, l), __builtin_amdgcn_readlane((int)(x >> 32), l));
+}
+// Inclusive prefix sums of 64-bit values over the wave, on the vector pipe.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t dpp64(int64_t x) {
+  return join64(__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false),
+                __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ int64_t wave_scan64(int64_t x) {
+  x += dpp64<0x111, 0xf>(x);  // row_shr:1, 2, 4, 8
+  x += dpp64<0x112, 0xf>(x);
+  x += dpp64<0x114, 0xf>(x);
+  x += dpp64<0x118, 0xf>(x);
+  x += dpp64<0x142, 0xa>(x);  // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+  x += dpp64<0x143, 0xc>(x);
+  return x;
+}
+// y / c of non-negative numbers (uniform): almost always both have 32 bits, where a division is much shorter.
+__device__ __forceinline__ int64_t quotient(int64_t y, int64_t c) {
+  if ((uint64_t)(y | c) >> 32 == 0) return (uint32_t)y / (uint32_t)c;
+  return y / c;
 }
 
 // The line of all work, seen by one wave: lane i sums the sequences [i * chunk, (i + 1) * chunk).
@@ -111,17 +123,30 @@ struct Line {
   int chunk;
   int64_t incl, sum;  // of the lane's sequences and all before them; of the lane's alone
   int64_t total;
+  int m, n, row0;     // chunk 1: the lane's sequence
 
   __device__ __forceinline__ void init(const PagedArgs& a) {
     const int lane = threadIdx.x & 63;
     chunk = (a.batch + 63) >> 6;
     sum = 0;
+    m = n = row0 = 0;
     const int64_t b0 = (int64_t)lane * chunk;
     for (int i = 0; i < chunk; ++i)
-      if (b0 + i < a.batch) sum += seq_work<QT>(a, (int)b0 + i).cost;
+      if (b0 + i < a.batch) {
+        const SeqWork s = read_work<QT>(a, (int)b0 + i);
+        sum += s.cost;
+        m = s.m; n = s.n; row0 = s.row0;
+      }
     sum *= a.kv_heads;
     incl = wave_scan64(sum);
     total = lane64(incl, 63);
+  }
+
+  // The work of sequence b (uniform): from the lane that has read it already where every lane has one.
+  __device__ __forceinline__ SeqWork work(const PagedArgs& a, int b) const {
+    if (chunk > 1) return read_work<QT>(a, b);
+    return seq_work<QT>(a, __builtin_amdgcn_readlane(m, b), __builtin_amdgcn_readlane(n, b),
+                        __builtin_amdgcn_readlane(row0, b));
   }
 
   // (x < total)
@@ -133,7 +158,7 @@ struct Line {
     int b = l * chunk;
     for (int left = chunk; chunk > 1 && left > 0; left -= 64) {  // sequences b .. b + 63 of the lane's, one per lane
       int64_t c = 0;
-      if (lane < left && b + lane < a.batch) c = seq_work<QT>(a, b + lane).cost * a.kv_heads;
+      if (lane < left && b + lane < a.batch) c = read_work<QT>(a, b + lane).cost * a.kv_heads;
       const int64_t in = wave_scan64(c);
       const uint64_t p = __ballot(before + in <= x);
       const int j = __popcll(p);
@@ -147,19 +172,18 @@ struct Line {
     }
     Place r;
     r.b = __builtin_amdgcn_readfirstlane(b);
-    r.s = seq_work<QT>(a, r.b);
-    const int64_t rel = uniform64(x - before);
+    r.s = work(a, r.b);
     r.h = 0;
     r.t = 0;
-    int64_t y = rel;
+    int64_t y = uniform64(x - before);
     if (a.kv_heads > 1) {
-      r.h = (int)(y / r.s.cost);
+      r.h = (int)quotient(y, r.s.cost);
       y -= (int64_t)r.h * r.s.cost;
     }
     if (r.s.tiles > 1) {
       const bool causal = a.causal && !a.whole;
       if (!causal) {
-        r.t = (int)(y / r.s.base);
+        r.t = (int)quotient(y, r.s.base);
       } else {
         int lo = 0, hi = r.s.tiles;  // tiles_cost(lo) <= y < tiles_cost(hi)
         while (hi - lo > 1) {
@@ -173,21 +197,40 @@ struct Line {
     r.u = y;
     return r;
   }
+
+  // Moves on to the next tile of the line.
+  __device__ __forceinline__ void next(const PagedArgs& a, Place& p) const {
+    p.u = 0;
+    if (++p.t < p.s.tiles) return;
+    p.t = 0;
+    if (++p.h < a.kv_heads) return;
+    p.h = 0;
+    do {
+      if (++p.b >= a.batch) return;
+      p.s = work(a, p.b);
+    } while (p.s.cost == 0);
+  }
 };
 
 // The length of the line a worker takes, and the workers that get any.
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t total) {
   if (a.whole) return 1;
-  const int64_t s = (total + a.workers - 1) / a.workers, least = (int64_t)a.min_share * a.group;
+  const int64_t s = quotient(total + a.workers - 1, a.workers), least = (int64_t)a.min_share * a.group;
   return s > least ? s : least;
 }
 
 // Workers in the order of the line: consecutive ones, which may share keys (tiles of one head, one range), are put on one XCD.
-// Workgroups are dealt to the 8 XCDs in turn.
+// Workgroups are dealt to the 8 XCDs in turn.  (A permutation of the workers.)
 __device__ __forceinline__ int64_t worker_place(int w, int64_t active) {
   const int64_t per = (active + 7) >> 3;
-  return w < 8 * per ? (int64_t)(w & 7) * per + (w >> 3) : active;
+  return w < 8 * per ? (int64_t)(w & 7) * per + (w >> 3) : w;
 }
+
+// What the reduce kernel has to know of the tile that a worker began and did not finish.  Every worker writes one.
+struct CutTile {
+  int32_t parts;   // workers the tile reaches into, or 0: no such tile
+  int32_t pairs, pair0, head, row0, pad[3];
+};
 
 // One tile's part [u0, u1) of its cost, as keys [k0, k1).
 struct Segment {
@@ -219,7 +262,7 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
   }
   // (cuts lie at multiples of 32 keys; the part after a cut works the same key out)
   auto key = [&](int64_t u) {
-    const int64_t k = (u / a.group - TILE_KEYS) & ~(int64_t)31;
+    const int64_t k = (quotient(u, a.group) - TILE_KEYS) & ~(int64_t)31;
     return clampi(k, 0, g.vis);
   };
   g.k0 = g.first ? 0 : key(g.u0);
@@ -227,18 +270,18 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
   return g;
 }
 
-// Moves on to the next tile of the line.
-template <int QT>
-__device__ __forceinline__ void next_tile(const PagedArgs& a, Place& p) {
-  p.u = 0;
-  if (++p.t < p.s.tiles) return;
-  p.t = 0;
-  if (++p.h < a.kv_heads) return;
-  p.h = 0;
-  do {
-    if (++p.b >= a.batch) return;
-    p.s = seq_work<QT>(a, p.b);
-  } while (p.s.cost == 0);
+// The record of a tile whose part sg a worker has done, starting at place `at` of the line: parts == 0 unless it began there and goes on.
+__device__ __forceinline__ CutTile cut_tile(const PagedArgs& a, const Place& p, const Segment& sg, int64_t at, int64_t share,
+                                            int64_t w, int qt) {
+  CutTile c = {};
+  if (sg.first && !sg.last) {
+    c.parts = (int)(quotient(at + sg.cost - 1, share) - w) + 1;
+    c.pairs = sg.pairs;
+    c.pair0 = p.t * qt;
+    c.head = p.h;
+    c.row0 = p.s.row0;
+  }
+  return c;
 }
 
 // Page ids of a sequence, 64 at a time in the lanes of a register: ids outside the cache become -1 (such a page's rows count as

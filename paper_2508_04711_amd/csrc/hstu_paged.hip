@@ -362,21 +362,67 @@ __device__ __forceinline__ int out_element(int x, int g) {
   }
 }
 
-template <bool F32, int DQK, int DV, bool BIAS>
-__global__ void __launch_bounds__(64, 2) paged_few_kernel(PagedArgs a) {
+// Rounds and stores four neighbouring elements of an output row.
+__device__ __forceinline__ void store4(const PagedArgs& a, int64_t elem, float x0, float x1, float x2, float x3) {
+  const float scale = a.alpha * a.inv_n;
+  if (a.out_f32) {
+    *(float4*)((float*)a.o + elem) = make_float4(x0 * scale, x1 * scale, x2 * scale, x3 * scale);
+  } else {
+    bf16x4 z;
+    z[0] = (__bf16)(x0 * scale); z[1] = (__bf16)(x1 * scale); z[2] = (__bf16)(x2 * scale); z[3] = (__bf16)(x3 * scale);
+    *(bf16x4*)((__bf16*)a.o + elem) = z;
+  }
+}
+
+// Streams the keys [k0, k1) of head h of sequence b past the wave's pairs.
+template <class F>
+__device__ __forceinline__ void stream_keys(F& f, const PagedArgs& a, const TileCtx& t, int b, int h, int k0, int k1) {
+  if (k0 >= k1) return;
+  constexpr int BK = F::BK;
+  PageIds ids;
+  const int entries = (k1 + (1 << a.c.ps_log2) - 1) >> a.c.ps_log2;
+  ids.fill(a.c, b, k0 >> a.c.ps_log2, entries);
+  Rows16 r[F::PARTS];
+  auto where = [&](int key) {  // (behind the part's end: rows of no length, so that every path issues the same loads)
+    const bool more = key < k1;
+    if (more && !ids.holds((key + BK - 1) >> a.c.ps_log2)) ids.fill(a.c, b, key >> a.c.ps_log2, entries);
+    f.where(r, a.c, ids, h, more ? key : k0, more ? k1 : k0);
+  };
+  where(k0);
+  f.fetch_k(r);
+  f.fetch_v(r);
+  // K of the next block is loaded once this one's scores are made, V once it has been multiplied: a block and a half in flight
+  for (int key = k0; key < k1; key += BK) {
+    f.scores(t);
+    __builtin_amdgcn_sched_barrier(0);
+    where(key + BK);
+    f.fetch_k(r);
+    __builtin_amdgcn_sched_barrier(0);
+    f.values(t, key);
+    __builtin_amdgcn_sched_barrier(0);
+    f.fetch_v(r);
+  }
+}
+
+// NW = 1: workers are waves.  NW > 1: a worker is a workgroup whose waves share a tile's keys and add up their results in LDS.
+template <bool F32, int DQK, int DV, bool BIAS, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
   typedef Few<F32, DQK, DV, BIAS> F;
-  constexpr int BK = F::BK, ES = F32 ? 4 : 2;
+  constexpr int ES = F32 ? 4 : 2;
   __shared__ float wtab[BIAS ? MAX_TS_BUCKETS : 1];
-  const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
+  __shared__ float4 sums[NW > 1 ? NW * FEW_PAIRS * DV / 4 : 1];
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 
   Line<FEW_PAIRS> line;
   line.init(a);
-  if (line.total == 0) return;
-  const int64_t share = share_of(a, line.total), active = (line.total + share - 1) / share;
+  const int64_t share = share_of(a, line.total), active = quotient(line.total + share - 1, share);
   const int64_t w = worker_place(blockIdx.x, active);
-  if (w >= active) return;
+  if (w >= active) {
+    if (!a.whole && lane == 0) a.cut[w].parts = 0;
+    return;
+  }
   if constexpr (BIAS) {
-    for (int x = lane; x < a.nb; x += 64) wtab[x] = a.ts_w[x];
+    for (int x = threadIdx.x; x < a.nb; x += 64 * NW) wtab[x] = a.ts_w[x];
     __syncthreads();
   }
   int64_t at = w * share;
@@ -391,6 +437,7 @@ __global__ void __launch_bounds__(64, 2) paged_few_kernel(PagedArgs a) {
   t.nb = a.nb;
   t.f = a.f;
   t.tq = 0;
+  CutTile cut = {};
   while (at < end && pl.b < a.batch) {
     const Segment sg = make_segment<FEW_PAIRS>(a, pl.s, pl.t, pl.u, end - at);
     // the lane's pair
@@ -404,51 +451,41 @@ __global__ void __launch_bounds__(64, 2) paged_few_kernel(PagedArgs a) {
     t.lim = a.causal ? clampi((int64_t)pl.s.n - pl.s.m + row + 1, 0, pl.s.n) : pl.s.n;
     f.start(on ? a.q + qrow * a.q_stride + (int64_t)head * DQK * ES : nullptr);
 
-    if (sg.k0 < sg.k1) {
-      PageIds ids;
-      const int entries = (sg.k1 + (1 << a.c.ps_log2) - 1) >> a.c.ps_log2;
-      ids.fill(a.c, pl.b, sg.k0 >> a.c.ps_log2, entries);
-      Rows16 r[F::PARTS];
-      auto where = [&](int key) {  // (behind the part's end: rows of no length, so that every path issues the same loads)
-        const bool more = key < sg.k1;
-        if (more && !ids.holds((key + BK - 1) >> a.c.ps_log2)) ids.fill(a.c, pl.b, key >> a.c.ps_log2, entries);
-        f.where(r, a.c, ids, pl.h, more ? key : sg.k0, more ? sg.k1 : sg.k0);
-      };
-      where(sg.k0);
-      f.fetch_k(r);
-      f.fetch_v(r);
-      for (int key = sg.k0; key < sg.k1; key += BK) {
-        f.scores(t);
-        __builtin_amdgcn_sched_barrier(0);
-        where(key + BK);
-        f.fetch_k(r);
-        __builtin_amdgcn_sched_barrier(0);
-        f.values(t, key);
-        __builtin_amdgcn_sched_barrier(0);
-        f.fetch_v(r);
+    if constexpr (NW > 1) {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const int per = ((sg.k1 + 32 * NW - 1) / (32 * NW)) * 32, k0 = wave * per;  // (whole tiles: from key 0 on)
+      stream_keys(f, a, t, pl.b, pl.h, k0, k0 + per < sg.k1 ? k0 + per : sg.k1);
+      float x[F::OUT];
+      f.result(x);
+      float* slot = (float*)sums + (wave * FEW_PAIRS + i) * DV;
+      if (on)
+#pragma unroll
+        for (int y = 0; y < F::OUT; y += 4)
+          *(float4*)(slot + out_element<F32, DV>(y, g)) = make_float4(x[y], x[y + 1], x[y + 2], x[y + 3]);
+      __syncthreads();
+      for (int c = threadIdx.x; c < sg.pairs * (DV / 4); c += 64 * NW) {
+        float4 s = sums[c];
+#pragma unroll
+        for (int v = 1; v < NW; ++v) {
+          const float4 y = sums[v * FEW_PAIRS * DV / 4 + c];
+          s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
+        }
+        const int p = pl.t * FEW_PAIRS + c / (DV / 4);
+        const int64_t o = (int64_t)(pl.s.row0 + p / a.group) * a.heads + pl.h * a.group + p % a.group;
+        store4(a, o * DV + (c % (DV / 4)) * 4, s.x, s.y, s.z, s.w);
       }
+      return;  // (one tile)
     }
 
+    stream_keys(f, a, t, pl.b, pl.h, sg.k0, sg.k1);
     if (on) {
       float x[F::OUT];
       f.result(x);
       if (sg.first && sg.last) {
-        const float scale = a.alpha * a.inv_n;
         const int64_t elem = (qrow * a.heads + head) * DV;
-        if (a.out_f32) {
 #pragma unroll
-          for (int y = 0; y < F::OUT; y += 4)
-            *(float4*)((float*)a.o + elem + out_element<F32, DV>(y, g)) =
-                make_float4(x[y] * scale, x[y + 1] * scale, x[y + 2] * scale, x[y + 3] * scale);
-        } else {
-#pragma unroll
-          for (int y = 0; y < F::OUT; y += 4) {
-            bf16x4 z;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = (__bf16)(x[y + e] * scale);
-            *(bf16x4*)((__bf16*)a.o + elem + out_element<F32, DV>(y, g)) = z;
-          }
-        }
+        for (int y = 0; y < F::OUT; y += 4)
+          store4(a, elem + out_element<F32, DV>(y, g), x[y], x[y + 1], x[y + 2], x[y + 3]);
       } else {
         float* slot = a.partial + ((2 * w + (sg.first ? 1 : 0)) * FEW_PAIRS + i) * DV;
 #pragma unroll
@@ -456,45 +493,35 @@ __global__ void __launch_bounds__(64, 2) paged_few_kernel(PagedArgs a) {
           *(float4*)(slot + out_element<F32, DV>(y, g)) = make_float4(x[y], x[y + 1], x[y + 2], x[y + 3]);
       }
     }
+    cut = cut_tile(a, pl, sg, at, share, w, FEW_PAIRS);
     at += sg.u1 - sg.u0;
-    next_tile<FEW_PAIRS>(a, pl);
+    line.next(a, pl);
   }
+  if (!a.whole && lane == 0) a.cut[w] = cut;
 }
 
 // ---- sum of the parts ------------------------------------------------------------------------------------------------------
-// Workgroup w finds the tile that worker w began and did not finish (if there is one: workers work the same line out), and
-// adds up its parts: slot 2 w + 1, then slot 2 x of the workers x = w + 1, ... whose run the tile reaches into.
+// Workgroup w adds up the parts of the tile that worker w began and did not finish, if there is one: slot 2 w + 1, then slot 2 x of
+// the workers x = w + 1, ... that the tile reaches into.  Threads: one per four elements of the tile, in blockIdx.y blocks, and
+// where that leaves some over, runs of parts.
 constexpr int REDUCE_THREADS = 256;
 template <int QT, int DV>
 __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs a) {
   constexpr int RW = DV / 4;  // float4 of a row
   __shared__ float4 sums[REDUCE_THREADS];
-  Line<QT> line;
-  line.init(a);
-  if (line.total == 0) return;
-  const int64_t share = share_of(a, line.total), active = (line.total + share - 1) / share;
   const int64_t w = blockIdx.x;
-  const int64_t end = (w + 1) * share;
-  if (w >= active || end >= line.total) return;  // (the line's end is a tile's end)
-  // the tile that holds the run's last unit
-  const Place pl = line.find(a, end - 1);
-  const Segment sg = make_segment<QT>(a, pl.s, pl.t, pl.u, 1);
-  const int64_t tile0 = end - 1 - pl.u, tile1 = tile0 + sg.cost;
-  if (tile0 < w * share || tile1 <= end) return;  // begun before, or finished
-  const int parts = (int)((tile1 - 1) / share - w) + 1;
-
-  // threads: RW per row; rows and, where rows are few, runs of parts
-  const int cols = sg.pairs * RW;
+  const CutTile t = a.cut[w];
+  if (t.parts == 0) return;
+  const int cols = t.pairs * RW, tid = threadIdx.x;
   const int groups = cols >= REDUCE_THREADS ? 1 : REDUCE_THREADS / cols;
-  const int per = (parts + groups - 1) / groups;
-  const float scale = a.alpha * a.inv_n;
-  for (int c0 = 0; c0 < cols; c0 += REDUCE_THREADS) {
-    const int tid = threadIdx.x, grp = groups > 1 ? tid / cols : 0, c = groups > 1 ? tid % cols : c0 + tid;
+  const int per = (t.parts + groups - 1) / groups;
+  for (int c0 = blockIdx.y * REDUCE_THREADS; c0 < cols; c0 += gridDim.y * REDUCE_THREADS) {
+    const int grp = groups > 1 ? tid / cols : 0, c = groups > 1 ? tid % cols : c0 + tid;
     const bool on = grp < groups && c < cols;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (on) {
-      const int x1 = (grp + 1) * per < parts ? (grp + 1) * per : parts;
-#pragma unroll 4
+      const int x1 = (grp + 1) * per < t.parts ? (grp + 1) * per : t.parts;
+#pragma unroll 8
       for (int x = grp * per; x < x1; ++x) {
         const int64_t slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
         const float4 y = *(const float4*)(a.partial + slot * QT * DV + (int64_t)c * 4);
@@ -511,24 +538,24 @@ __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs 
         }
     }
     if (on && grp == 0) {
-      const int pair = pl.t * QT + c / RW, row = pair / a.group, head = pl.h * a.group + pair % a.group;
-      const int64_t elem = ((int64_t)(pl.s.row0 + row) * a.heads + head) * DV + (c % RW) * 4;
-      if (a.out_f32) {
-        *(float4*)((float*)a.o + elem) = make_float4(s.x * scale, s.y * scale, s.z * scale, s.w * scale);
-      } else {
-        bf16x4 z;
-        z[0] = (__bf16)(s.x * scale); z[1] = (__bf16)(s.y * scale); z[2] = (__bf16)(s.z * scale); z[3] = (__bf16)(s.w * scale);
-        *(bf16x4*)((__bf16*)a.o + elem) = z;
-      }
+      const int pair = t.pair0 + c / RW;
+      const int64_t o = (int64_t)(t.row0 + pair / a.group) * a.heads + t.head * a.group + pair % a.group;
+      store4(a, o * DV + (c % RW) * 4, s.x, s.y, s.z, s.w);
     }
   }
 }
 
+constexpr int TEAM = 8;
+template <bool F32, int DQK, int DV, int NW>
+hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)a.workers), block(64 * NW);
+  if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true, NW>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false, NW>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
 template <bool F32, int DQK, int DV>
 hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
-  if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true>), dim3((unsigned)a.workers), dim3(64), 0, stream, a);
-  else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false>), dim3((unsigned)a.workers), dim3(64), 0, stream, a);
-  return hipGetLastError();
+  return a.whole == 2 ? launch_few<F32, DQK, DV, TEAM>(a, stream) : launch_few<F32, DQK, DV, 1>(a, stream);
 }
 template <bool F32, int DQK>
 hipError_t launch_few_dv(const PagedArgs& a, int d_v, hipStream_t stream) {
@@ -542,7 +569,7 @@ hipError_t launch_few_d(const PagedArgs& a, int d_qk, int d_v, hipStream_t strea
 }
 template <int QT>
 hipError_t launch_reduce(const PagedArgs& a, int d_v, hipStream_t stream) {
-  const dim3 grid((unsigned)a.workers), block(REDUCE_THREADS);
+  const dim3 grid((unsigned)a.workers, QT > FEW_PAIRS ? 4 : 1), block(REDUCE_THREADS);
   if (d_v == 32) hipLaunchKernelGGL((paged_reduce_kernel<QT, 32>), grid, block, 0, stream, a);
   else if (d_v == 64) hipLaunchKernelGGL((paged_reduce_kernel<QT, 64>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((paged_reduce_kernel<QT, 128>), grid, block, 0, stream, a);

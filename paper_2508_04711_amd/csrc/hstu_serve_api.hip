@@ -84,13 +84,15 @@ PagedView view_of(const hstu_paged_cache* c) {
 
 // How the attention's work is divided (see hstu_paged.h).
 struct Division {
-  bool many, whole;
-  int workers, min_share;
-  size_t bytes;  // of partial results
+  bool many;
+  int whole, workers, min_share;
+  size_t front, bytes;  // records of cut tiles; these and partial results
 };
 constexpr int FEW_WORKERS = 2048;   // two one-wave workers per SIMD
 constexpr int MIN_SHARE = 64;       // keys that are worth a worker
-constexpr int WHOLE_KEYS = 256;     // up to that many keys a tile is one worker's, uncut
+constexpr int WHOLE_KEYS = 128;     // up to that many keys a tile is one worker's, uncut
+constexpr int TEAM_KEYS = 1024;     // ... where the worker is a team of waves
+constexpr int TEAM_TILES = 512;     // and that many tiles
 
 // false: sizes out of range
 bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division* d) {
@@ -101,16 +103,17 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   const int64_t tiles = pairs / qt + (c->batch < p->new_rows ? c->batch : p->new_rows);  // (of one head; at most)
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
-  const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap;
-  d->whole = keys <= WHOLE_KEYS && tiles * c->num_kv_heads < (1ll << 30);
+  const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap, all = tiles * c->num_kv_heads;
+  d->whole = keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0);
   d->min_share = MIN_SHARE;
-  int64_t workers = tiles * c->num_kv_heads;
+  int64_t workers = all;
   if (!d->whole) {
-    const double all = (double)workers * (double)(keys + 2 * TILE_KEYS) / MIN_SHARE + 1.0;
-    workers = all < FEW_WORKERS ? (int64_t)all : FEW_WORKERS;
+    const double most = (double)all * (double)(keys + 2 * TILE_KEYS) / MIN_SHARE + 1.0;
+    workers = most < FEW_WORKERS ? (int64_t)most : FEW_WORKERS;
   }
   d->workers = (int)((workers + 7) / 8 * 8);
-  d->bytes = d->whole ? 0 : (size_t)d->workers * 2 * (size_t)qt * c->d_v * sizeof(float);
+  d->front = d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256);
+  d->bytes = d->whole ? 0 : d->front + (size_t)d->workers * 2 * (size_t)qt * c->d_v * sizeof(float);
   return true;
 }
 
@@ -236,7 +239,8 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
     a.nb = bias->num_buckets; a.f = bias->groups_log2;
   }
   a.o = o;
-  a.partial = (float*)workspace;
+  a.cut = (CutTile*)workspace;
+  a.partial = (float*)((char*)workspace + d.front);
   a.batch = cache->batch; a.rows = (int32_t)params->new_rows;
   a.heads = params->num_heads; a.kv_heads = cache->num_kv_heads; a.group = params->num_heads / cache->num_kv_heads;
   a.causal = params->causal ? 1 : 0;
