@@ -96,6 +96,17 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 __device__ __forceinline__ int64_t lane64(int64_t x, int l) {
   return join64(__builtin_amdgcn_readlane((int)(uint32_t)x, l), __builtin_amdgcn_readlane((int)(x >> 32), l));
 }
+__device__ __forceinline__ int uniform32(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// What the compiler cannot see to be the same in all lanes it keeps in vector registers, and loops over the lanes to make a
+// buffer descriptor of it.
+__device__ __forceinline__ Place uniform_place(const Place& p) {
+  Place r;
+  r.b = uniform32(p.b); r.h = uniform32(p.h); r.t = uniform32(p.t);
+  r.u = uniform64(p.u);
+  r.s.m = uniform32(p.s.m); r.s.n = uniform32(p.s.n); r.s.row0 = uniform32(p.s.row0); r.s.tiles = uniform32(p.s.tiles);
+  r.s.base = uniform64(p.s.base); r.s.cost = uniform64(p.s.cost);
+  return r;
+}
 // Inclusive prefix sums of 64-bit values over the wave, on the vector pipe.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int64_t dpp64(int64_t x) {
@@ -118,7 +129,8 @@ __device__ __forceinline__ int64_t quotient(int64_t y, int64_t c) {
 }
 
 // The line of all work, seen by one wave: lane i sums the sequences [i * chunk, (i + 1) * chunk).
-template <int QT>
+// HELD: where every lane has one sequence only, it is kept (three registers) and not read again.
+template <int QT, bool HELD>
 struct Line {
   int chunk;
   int64_t incl, sum;  // of the lane's sequences and all before them; of the lane's alone
@@ -144,13 +156,16 @@ struct Line {
 
   // The work of sequence b (uniform): from the lane that has read it already where every lane has one.
   __device__ __forceinline__ SeqWork work(const PagedArgs& a, int b) const {
-    if (chunk > 1) return read_work<QT>(a, b);
+    if (!HELD || chunk > 1) return read_work<QT>(a, b);
     return seq_work<QT>(a, __builtin_amdgcn_readlane(m, b), __builtin_amdgcn_readlane(n, b),
                         __builtin_amdgcn_readlane(row0, b));
   }
 
   // (x < total)
   __device__ __forceinline__ Place find(const PagedArgs& a, int64_t x) const {
+    return uniform_place(find_place(a, x));
+  }
+  __device__ __forceinline__ Place find_place(const PagedArgs& a, int64_t x) const {
     const int lane = threadIdx.x & 63;
     const uint64_t past = __ballot(incl <= x);
     const int l = __popcll(past);  // first lane whose sum reaches beyond x
@@ -200,6 +215,10 @@ struct Line {
 
   // Moves on to the next tile of the line.
   __device__ __forceinline__ void next(const PagedArgs& a, Place& p) const {
+    next_place(a, p);
+    p = uniform_place(p);
+  }
+  __device__ __forceinline__ void next_place(const PagedArgs& a, Place& p) const {
     p.u = 0;
     if (++p.t < p.s.tiles) return;
     p.t = 0;
@@ -216,7 +235,7 @@ struct Line {
 __device__ __forceinline__ int64_t share_of(const PagedArgs& a, int64_t total) {
   if (a.whole) return 1;
   const int64_t s = quotient(total + a.workers - 1, a.workers), least = (int64_t)a.min_share * a.group;
-  return s > least ? s : least;
+  return uniform64(s > least ? s : least);
 }
 
 // Workers in the order of the line: consecutive ones, which may share keys (tiles of one head, one range), are put on one XCD.
@@ -265,8 +284,12 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
     const int64_t k = (quotient(u, a.group) - TILE_KEYS) & ~(int64_t)31;
     return clampi(k, 0, g.vis);
   };
-  g.k0 = g.first ? 0 : key(g.u0);
-  g.k1 = g.last ? g.vis : key(g.u1);
+  g.k0 = uniform32(g.first ? 0 : key(g.u0));
+  g.k1 = uniform32(g.last ? g.vis : key(g.u1));
+  g.lim0 = uniform32(g.lim0);
+  g.vis = uniform32(g.vis);
+  g.pairs = uniform32(g.pairs);
+  g.u1 = uniform64(g.u1);
   return g;
 }
 
@@ -282,6 +305,13 @@ __device__ __forceinline__ CutTile cut_tile(const PagedArgs& a, const Place& p, 
     c.row0 = p.s.row0;
   }
   return c;
+}
+
+// Rows of the 16 from `key` on that lie before `end`, none without a page.  (In a scalar register: the clamp is a vector
+// instruction, and a descriptor made of its result would be a loop over the lanes.)
+__device__ __forceinline__ int rows_before(int id, int key, int end) {
+  const int left = end - key;
+  return uniform32(id < 0 || left < 0 ? 0 : (left < 16 ? left : 16));
 }
 
 // Page ids of a sequence, 64 at a time in the lanes of a register: ids outside the cache become -1 (such a page's rows count as

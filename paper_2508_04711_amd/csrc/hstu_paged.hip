@@ -72,8 +72,7 @@ __device__ __forceinline__ Rows16 rows16(const PagedView& c, const PageIds& ids,
   r.k = c.k + page * c.k_page + row * ROW_K;
   r.v = c.v + page * c.v_page + row * ROW_V;
   r.ts = c.ts + (page << c.ps_log2) + slot;
-  const int left = end - key;
-  r.n = id < 0 || left < 0 ? 0 : (left < 16 ? left : 16);
+  r.n = rows_before(id, key, end);
   return r;
 }
 
@@ -413,10 +412,10 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
   __shared__ float4 sums[NW > 1 ? NW * FEW_PAIRS * DV / 4 : 1];
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 
-  Line<FEW_PAIRS> line;
+  Line<FEW_PAIRS, true> line;
   line.init(a);
-  const int64_t share = share_of(a, line.total), active = quotient(line.total + share - 1, share);
-  const int64_t w = worker_place(blockIdx.x, active);
+  const int64_t share = share_of(a, line.total), active = uniform64(quotient(line.total + share - 1, share));
+  const int64_t w = uniform64(worker_place(blockIdx.x, active));
   if (w >= active) {
     if (!a.whole && lane == 0) a.cut[w].parts = 0;
     return;

@@ -88,6 +88,9 @@ struct Division {
   int whole, workers, min_share;
   size_t front, bytes;  // records of cut tiles; these and partial results
 };
+constexpr int MANY_MEAN = 24;       // pairs per sequence and key/value head from which on the matrix cores bound the pass
+constexpr int MANY_WORKERS = 512;   // two workgroups per CU
+constexpr int MANY_SHARE = 128;
 constexpr int FEW_WORKERS = 2048;   // two one-wave workers per SIMD
 constexpr int MIN_SHARE = 64;       // keys that are worth a worker
 constexpr int WHOLE_KEYS = 128;     // up to that many keys a tile is one worker's, uncut
@@ -98,18 +101,19 @@ constexpr int TEAM_TILES = 512;     // and that many tiles
 bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division* d) {
   const int group = p->num_heads / c->num_kv_heads;
   const int64_t cap = view_of(c).cap, pairs = p->new_rows * group;
-  d->many = false;
+  d->many = c->dtype == HSTU_BF16 && pairs > (int64_t)MANY_MEAN * c->batch;
   const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS;
   const int64_t tiles = pairs / qt + (c->batch < p->new_rows ? c->batch : p->new_rows);  // (of one head; at most)
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
   const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap, all = tiles * c->num_kv_heads;
-  d->whole = keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0);
-  d->min_share = MIN_SHARE;
+  d->whole = d->many ? 0 : (keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
+  d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
   int64_t workers = all;
   if (!d->whole) {
-    const double most = (double)all * (double)(keys + 2 * TILE_KEYS) / MIN_SHARE + 1.0;
-    workers = most < FEW_WORKERS ? (int64_t)most : FEW_WORKERS;
+    const double most = (double)all * (double)(keys + 2 * TILE_KEYS) / d->min_share + 1.0;
+    const int limit = d->many ? MANY_WORKERS : FEW_WORKERS;
+    workers = most < limit ? (int64_t)most : limit;
   }
   d->workers = (int)((workers + 7) / 8 * 8);
   d->front = d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256);
@@ -250,7 +254,9 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   {
     TimedLaunch timed(16, stream);
-    if (launch_paged_few(a, cache->dtype == HSTU_F32, cache->d_qk, cache->d_v, stream) != hipSuccess) return HSTU_ERR_HIP;
+    const hipError_t e = d.many ? launch_paged_many(a, cache->d_qk, cache->d_v, stream)
+                                : launch_paged_few(a, cache->dtype == HSTU_F32, cache->d_qk, cache->d_v, stream);
+    if (e != hipSuccess) return HSTU_ERR_HIP;
   }
   if (d.whole) return HSTU_OK;
   TimedLaunch timed(17, stream);
