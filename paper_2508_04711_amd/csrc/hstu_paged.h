@@ -34,7 +34,9 @@ struct PagedArgs {
   int32_t batch, rows, heads, kv_heads, group;
   int32_t causal, out_f32;
   float alpha, inv_n;
-  int32_t workers;            // a multiple of 8
+  int32_t workers;            // a multiple of 8; many rows: the units that the work is cut into, about
+  int32_t records;            // many rows: records of cut tiles that there is room for
+  int32_t grid;               // workgroups: enough for all workers or units
   int32_t whole;              // 1: every worker takes one tile, uncut; 2: ... and is a team of waves
   int32_t min_share;          // keys a worker takes at least
 };
@@ -129,8 +131,7 @@ __device__ __forceinline__ int64_t quotient(int64_t y, int64_t c) {
 }
 
 // The line of all work, seen by one wave: lane i sums the sequences [i * chunk, (i + 1) * chunk).
-// HELD: where every lane has one sequence only, it is kept (three registers) and not read again.
-template <int QT, bool HELD>
+template <int QT>
 struct Line {
   int chunk;
   int64_t incl, sum;  // of the lane's sequences and all before them; of the lane's alone
@@ -156,7 +157,7 @@ struct Line {
 
   // The work of sequence b (uniform): from the lane that has read it already where every lane has one.
   __device__ __forceinline__ SeqWork work(const PagedArgs& a, int b) const {
-    if (!HELD || chunk > 1) return read_work<QT>(a, b);
+    if (chunk > 1) return read_work<QT>(a, b);
     return seq_work<QT>(a, __builtin_amdgcn_readlane(m, b), __builtin_amdgcn_readlane(n, b),
                         __builtin_amdgcn_readlane(row0, b));
   }
@@ -245,10 +246,12 @@ __device__ __forceinline__ int64_t worker_place(int w, int64_t active) {
   return w < 8 * per ? (int64_t)(w & 7) * per + (w >> 3) : w;
 }
 
-// What the reduce kernel has to know of the tile that a worker began and did not finish.  Every worker writes one.
+// What the reduce kernel has to know of a cut tile: its parts are in slots slot0 and next, next + step, ...  Few rows: every worker
+// writes a record, of the tile that it began and did not finish.
 struct CutTile {
-  int32_t parts;   // workers the tile reaches into, or 0: no such tile
-  int32_t pairs, pair0, head, row0, pad[3];
+  int32_t parts;   // or 0: no such tile
+  int32_t pairs, pair0, head, row0;
+  int32_t slot0, next, step;
 };
 
 // One tile's part [u0, u1) of its cost, as keys [k0, k1).
@@ -293,6 +296,166 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
   return g;
 }
 
+// ---- the schedule of calls of many rows ----------------------------------------------------------------------------------
+// There the tiles of one head read the same keys several times over, and what bounds the pass is whether they find them in
+// their XCD's L2: workers that run side by side have to stream the same keys at the same time.  So all tiles of a head are
+// cut at the same keys, into C pieces each (C: its sequence's length over a common share), units are ordered sequence, head,
+// piece, tile, and every workgroup takes one unit.  The share is the smallest with which every unit runs at once:
+// more units would be a second round of the chip for a few, and more partial results, of 64 KB each at d_v = 128.
+struct ManyUnit {
+  int b, m, n, row0, tiles;
+  int h, t;
+  int k0, k1;      // keys of the unit, k1 <= vis
+  int lim0, vis;   // keys that the tile's first and last row see
+  int pairs;
+  int parts;       // pieces of this tile that see any keys (1: uncut)
+  int piece;
+  int slot, cut;   // where the sequence's tiles are cut: the unit's slot, the tile's record (else -1)
+};
+
+template <int QT>
+struct Units {
+  int chunk, share;
+  int m, n, row0;                    // chunk 1: the lane's sequence
+  int units, cut_units, cut_tiles;   // of the lane's sequences and all before them
+  int lane_units, lane_cut_units, lane_cut_tiles;
+  int total, total_cut;
+
+  struct Counts { int pieces, units, cut_units, cut_tiles; };
+  __device__ __forceinline__ Counts counts(const PagedArgs& a, int m_, int n_) const {
+    const int tiles = (int)(((int64_t)m_ * a.group + QT - 1) / QT);
+    Counts c;
+    c.pieces = !a.whole && n_ > share ? (int)(((int64_t)n_ + share - 1) / share) : 1;
+    c.units = tiles * c.pieces * a.kv_heads;
+    c.cut_units = c.pieces > 1 ? c.units : 0;
+    c.cut_tiles = c.pieces > 1 ? tiles * a.kv_heads : 0;
+    return c;
+  }
+  __device__ __forceinline__ void read(const PagedArgs& a, int b, int& m_, int& n_, int& r) const {
+    int e;
+    seq_range(a.off, b, a.rows, r, e);
+    m_ = e - r;
+    n_ = clampi(a.c.lens[b], 0, a.c.cap);
+  }
+
+  __device__ __forceinline__ void init(const PagedArgs& a) {
+    const int lane = threadIdx.x & 63;
+    chunk = (a.batch + 63) >> 6;
+    m = n = row0 = 0;
+    const int64_t b0 = (int64_t)lane * chunk;
+    int64_t keys = 0;
+    int tiles = 0;
+    for (int i = 0; i < chunk; ++i)
+      if (b0 + i < a.batch) {
+        read(a, (int)b0 + i, m, n, row0);
+        const int t = (int)(((int64_t)m * a.group + QT - 1) / QT);
+        tiles += t;
+        keys += t * (int64_t)n;
+      }
+    const int all_tiles = __builtin_amdgcn_readlane(wave_scan(tiles), 63) * a.kv_heads;
+    const int64_t all = lane64(wave_scan64(keys), 63) * a.kv_heads;
+    share = find_share(a, tiles, all_tiles, all);
+    lane_units = lane_cut_units = lane_cut_tiles = 0;
+    for (int i = 0; i < chunk; ++i)
+      if (b0 + i < a.batch) {
+        if (chunk > 1) read(a, (int)b0 + i, m, n, row0);
+        const Counts c = counts(a, m, n);
+        lane_units += c.units;
+        lane_cut_units += c.cut_units;
+        lane_cut_tiles += c.cut_tiles;
+      }
+    units = wave_scan(lane_units);
+    cut_units = wave_scan(lane_cut_units);
+    cut_tiles = wave_scan(lane_cut_tiles);
+    total = __builtin_amdgcn_readlane(units, 63);
+    total_cut = __builtin_amdgcn_readlane(cut_tiles, 63);
+  }
+
+  // The smallest share whose units have a place each in the chip's `workers` at once; where the tiles alone fill three quarters of
+  // them, in two rounds; where they fill more than most of two rounds, what one worker does of all the keys (only the
+  // longest sequences are then cut).
+  __device__ __forceinline__ int find_share(const PagedArgs& a, int tiles, int all_tiles, int64_t all) const {
+    const int room = 4 * all_tiles <= 3 * a.workers ? a.workers : 2 * a.workers;
+    const bool fit = 8 * (int64_t)all_tiles <= 7 * (int64_t)room;
+    // units <= keys / share + tiles
+    int64_t hi = fit ? quotient(all, room - all_tiles) + 64 : quotient(all, a.workers) + 1, lo = quotient(all, room);
+    if (fit && chunk == 1)
+      while (hi - lo > 64) {
+        const uint32_t mid = (uint32_t)((lo + hi) / 2);
+        const int u = __builtin_amdgcn_readlane(wave_scan(tiles * (int)(((uint32_t)n + mid - 1) / mid)), 63) * a.kv_heads;
+        if (u <= room) hi = mid; else lo = mid;
+      }
+    return uniform32((int)(hi > a.min_share ? (hi < 0x7fffffc0 ? hi : 0x7fffffc0) : a.min_share));
+  }
+
+  // (u < total)
+  __device__ __forceinline__ ManyUnit find(const PagedArgs& a, int u) const {
+    const int lane = threadIdx.x & 63;
+    const int l = __popcll(__ballot(units <= u));
+    int before = __builtin_amdgcn_readlane(units - lane_units, l);
+    int slots = __builtin_amdgcn_readlane(cut_units - lane_cut_units, l);
+    int cuts = __builtin_amdgcn_readlane(cut_tiles - lane_cut_tiles, l);
+    ManyUnit r;
+    int b = l * chunk;
+    r.b = b;
+    if (chunk == 1) {
+      r.m = __builtin_amdgcn_readlane(m, l);
+      r.n = __builtin_amdgcn_readlane(n, l);
+      r.row0 = __builtin_amdgcn_readlane(row0, l);
+    } else {
+      for (int left = chunk; left > 0; left -= 64) {  // sequences b .. b + 63 of the lane's, one per lane
+        Counts c = {};
+        int m_ = 0, n_ = 0, r_ = 0;
+        if (lane < left && b + lane < a.batch) {
+          read(a, b + lane, m_, n_, r_);
+          c = counts(a, m_, n_);
+        }
+        const int iu = wave_scan(c.units), is = wave_scan(c.cut_units), ic = wave_scan(c.cut_tiles);
+        const int j = __popcll(__ballot(before + iu <= u));
+        if (j < 64) {
+          before += __builtin_amdgcn_readlane(iu - c.units, j);
+          slots += __builtin_amdgcn_readlane(is - c.cut_units, j);
+          cuts += __builtin_amdgcn_readlane(ic - c.cut_tiles, j);
+          r.b = b + j;
+          r.m = __builtin_amdgcn_readlane(m_, j);
+          r.n = __builtin_amdgcn_readlane(n_, j);
+          r.row0 = __builtin_amdgcn_readlane(r_, j);
+          break;
+        }
+        before += __builtin_amdgcn_readlane(iu, 63);
+        slots += __builtin_amdgcn_readlane(is, 63);
+        cuts += __builtin_amdgcn_readlane(ic, 63);
+        b += 64;
+      }
+    }
+    r.b = uniform32(r.b);
+    r.tiles = uniform32((int)(((int64_t)r.m * a.group + QT - 1) / QT));
+    const int pieces = uniform32(counts(a, r.m, r.n).pieces);
+    const uint32_t rel = u - before, per_head = (uint32_t)r.tiles * pieces;
+    r.h = uniform32(rel / per_head);
+    const uint32_t x = rel - r.h * per_head;
+    r.piece = uniform32(x / r.tiles);
+    r.t = uniform32(x - r.piece * r.tiles);
+    const int64_t p0 = (int64_t)r.t * QT, all = (int64_t)r.m * a.group;
+    r.pairs = uniform32(all - p0 < QT ? (int)(all - p0) : QT);
+    r.lim0 = r.vis = r.n;
+    if (a.causal) {
+      const int64_t past = (int64_t)r.n - r.m + 1;
+      r.lim0 = uniform32(clampi(past + (int)((uint32_t)p0 / a.group), 0, r.n));
+      r.vis = uniform32(clampi(past + (int)((uint32_t)(p0 + r.pairs - 1) / a.group), 0, r.n));
+    }
+    const int size = uniform32((int)((((int64_t)r.n + pieces - 1) / pieces + 63) & ~63ll));  // keys of a piece
+    const int64_t k0 = (int64_t)r.piece * size;
+    r.k0 = uniform32(k0 < r.vis ? (int)k0 : r.vis);
+    r.k1 = uniform32(k0 + size < r.vis ? (int)(k0 + size) : r.vis);
+    const int parts = r.vis > size ? (int)(((int64_t)r.vis + size - 1) / size) : 1;
+    r.parts = uniform32(pieces > 1 ? parts : 1);
+    r.slot = slots + (int)rel;
+    r.cut = pieces > 1 ? cuts + r.h * r.tiles + r.t : -1;
+    return r;
+  }
+};
+
 // The record of a tile whose part sg a worker has done, starting at place `at` of the line: parts == 0 unless it began there and goes on.
 __device__ __forceinline__ CutTile cut_tile(const PagedArgs& a, const Place& p, const Segment& sg, int64_t at, int64_t share,
                                             int64_t w, int qt) {
@@ -303,6 +466,9 @@ __device__ __forceinline__ CutTile cut_tile(const PagedArgs& a, const Place& p, 
     c.pair0 = p.t * qt;
     c.head = p.h;
     c.row0 = p.s.row0;
+    c.slot0 = (int)(2 * w + 1);
+    c.next = (int)(2 * w + 2);
+    c.step = 2;
   }
   return c;
 }

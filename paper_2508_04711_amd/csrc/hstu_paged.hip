@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
   __shared__ float4 sums[NW > 1 ? NW * FEW_PAIRS * DV / 4 : 1];
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
 
-  Line<FEW_PAIRS, true> line;
+  Line<FEW_PAIRS> line;
   line.init(a);
   const int64_t share = share_of(a, line.total), active = uniform64(quotient(line.total + share - 1, share));
   const int64_t w = uniform64(worker_place(blockIdx.x, active));
@@ -500,16 +500,14 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
 }
 
 // ---- sum of the parts ------------------------------------------------------------------------------------------------------
-// Workgroup w adds up the parts of the tile that worker w began and did not finish, if there is one: slot 2 w + 1, then slot 2 x of
-// the workers x = w + 1, ... that the tile reaches into.  Threads: one per four elements of the tile, in blockIdx.y blocks, and
-// where that leaves some over, runs of parts.
-constexpr int REDUCE_THREADS = 256;
+// Workgroup w adds up the parts of the tile of record w, if there is one, in their order.  Threads: one per four elements of the tile, in
+// blockIdx.y blocks, and where that leaves some over, runs of parts.
+constexpr int REDUCE_THREADS = 256, REDUCE_SPLIT = 16;  // (many rows: workgroups per tile)
 template <int QT, int DV>
 __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs a) {
   constexpr int RW = DV / 4;  // float4 of a row
   __shared__ float4 sums[REDUCE_THREADS];
-  const int64_t w = blockIdx.x;
-  const CutTile t = a.cut[w];
+  const CutTile t = a.cut[blockIdx.x];
   if (t.parts == 0) return;
   const int cols = t.pairs * RW, tid = threadIdx.x;
   const int groups = cols >= REDUCE_THREADS ? 1 : REDUCE_THREADS / cols;
@@ -522,7 +520,7 @@ __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs 
       const int x1 = (grp + 1) * per < t.parts ? (grp + 1) * per : t.parts;
 #pragma unroll 8
       for (int x = grp * per; x < x1; ++x) {
-        const int64_t slot = x == 0 ? 2 * w + 1 : 2 * (w + x);
+        const int64_t slot = x == 0 ? t.slot0 : t.next + (int64_t)(x - 1) * t.step;
         const float4 y = *(const float4*)(a.partial + slot * QT * DV + (int64_t)c * 4);
         s.x += y.x; s.y += y.y; s.z += y.z; s.w += y.w;
       }
@@ -547,7 +545,7 @@ __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs 
 constexpr int TEAM = 8;
 template <bool F32, int DQK, int DV, int NW>
 hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.workers), block(64 * NW);
+  const dim3 grid((unsigned)a.grid), block(64 * NW);
   if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true, NW>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false, NW>), grid, block, 0, stream, a);
   return hipGetLastError();
@@ -568,7 +566,7 @@ hipError_t launch_few_d(const PagedArgs& a, int d_qk, int d_v, hipStream_t strea
 }
 template <int QT>
 hipError_t launch_reduce(const PagedArgs& a, int d_v, hipStream_t stream) {
-  const dim3 grid((unsigned)a.workers, QT > FEW_PAIRS ? 4 : 1), block(REDUCE_THREADS);
+  const dim3 grid((unsigned)(QT > FEW_PAIRS ? a.records : a.workers), QT > FEW_PAIRS ? REDUCE_SPLIT : 1), block(REDUCE_THREADS);
   if (d_v == 32) hipLaunchKernelGGL((paged_reduce_kernel<QT, 32>), grid, block, 0, stream, a);
   else if (d_v == 64) hipLaunchKernelGGL((paged_reduce_kernel<QT, 64>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((paged_reduce_kernel<QT, 128>), grid, block, 0, stream, a);

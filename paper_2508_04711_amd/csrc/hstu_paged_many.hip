@@ -2,9 +2,8 @@
 //
 // With r (new row, query head) pairs per key/value head a row of the cache is worth r flops a byte: from about 128 on the
 // matrix cores bound the pass and not the memory.  So a worker is a workgroup of four waves, 32 pairs each, which shares the tiles
-// of 64 keys it streams through LDS: the forward pass's step (hstu_fwd_step.h) over pages.  Work is divided
-// as for few rows (hstu_paged.h): tiles of 128 pairs, cut along the keys at any multiple of 32, so a call of two tiles fills the chip
-// as one of hundreds does.
+// of 64 keys it streams through LDS: the forward pass's step (hstu_fwd_step.h) over pages.  Tiles of
+// 128 pairs are cut along the keys (Units, hstu_paged.h), so a call of two tiles fills the chip as one of hundreds does.
 //   - A wave-wide copy fills rows of one group of 16, which lies inside one page: its buffer descriptor is the group's
 //     rows, in scalar registers, and what lies behind the part's end or in a page that does not exist arrives as zeros.
 //   - The tiles of keys that every pair sees go through the pipelined step without any mask; the last few, which the causal
@@ -83,258 +82,244 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Line<MANY_PAIRS, false> line;
-  line.init(a);
-  const int64_t share = share_of(a, line.total), active = uniform64(quotient(line.total + share - 1, share));
-  const int64_t w = uniform64(worker_place(blockIdx.x, active));
-  if (w >= active) {
-    if (tid == 0) a.cut[w].parts = 0;
-    return;
-  }
+  Units<MANY_PAIRS> units;
+  units.init(a);
+  if (blockIdx.x == 0)  // (records that no tile uses)
+    for (int x = units.total_cut + tid; x < a.records; x += MANY_WAVES * 64) a.cut[x].parts = 0;
+  const int64_t w = worker_place(blockIdx.x, units.total);
+  if (w >= units.total) return;
   if constexpr (BIAS)
     for (int x = tid; x < a.nb; x += MANY_WAVES * 64) wtab[x] = a.ts_w[x];
-  int64_t at = w * share;
-  const int64_t end = at + share < line.total ? at + share : line.total;
-  Place pl = line.find(a, at);
+  const ManyUnit sg = units.find(a, uniform32((int)w));
+  if (sg.cut >= 0 && sg.piece == 0 && tid == 0) {
+    CutTile c = {};
+    c.parts = sg.parts > 1 ? sg.parts : 0;
+    c.pairs = sg.pairs; c.pair0 = sg.t * MANY_PAIRS; c.head = sg.h; c.row0 = sg.row0;
+    c.slot0 = sg.slot; c.next = sg.slot + sg.tiles; c.step = sg.tiles;
+    a.cut[sg.cut] = c;
+  }
+  if (sg.piece >= sg.parts) return;  // (keys that no row of the tile sees)
 
   RowAddr<DQK> ra;
   ColAddr<DV> ca;
   ra.init(n, hh);
   ca.init(lane);
   const float c1 = -a.alpha * 1.4426950408889634f;
-  CutTile cut = {};
-  while (at < end && pl.b < a.batch) {
-    const Segment sg = make_segment<MANY_PAIRS>(a, pl.s, pl.t, pl.u, end - at);
-    int ln = lane;
-    asm volatile("" : "+v"(ln));  // (what depends on the lane is worked out per tile, not kept over the pipelined loop)
-    const int slot = wave * 32 + (ln & 31);  // the lane's pair in the tile
-    const bool on = slot < sg.pairs;
-    const int pair = pl.t * MANY_PAIRS + slot, row = pair / a.group, head = pl.h * a.group + pair % a.group;
-    const int64_t qrow = pl.s.row0 + row;
-    bf16x8 qreg[DQK / 16];
+  const int slot = wave * 32 + n;  // the lane's pair in the tile
+  const int pair = sg.t * MANY_PAIRS + slot, row = pair / a.group, head = sg.h * a.group + pair % a.group;
+  const bool on = slot < sg.pairs, wave_on = wave * 32 < sg.pairs;
+  const int64_t qrow = sg.row0 + row;
+  bf16x8 qreg[DQK / 16];
 #pragma unroll
-    for (int s = 0; s < DQK / 16; ++s) {
-      u32x4 z = {0, 0, 0, 0};
-      if (on) z = *(const u32x4*)(a.q + qrow * a.q_stride + (int64_t)head * DQK * 2 + s * 32 + (ln >> 5) * 16);
-      qreg[s] = __builtin_bit_cast(bf16x8, z);
+  for (int s = 0; s < DQK / 16; ++s) {
+    u32x4 z = {0, 0, 0, 0};
+    if (on) z = *(const u32x4*)(a.q + qrow * a.q_stride + (int64_t)head * DQK * 2 + s * 32 + hh * 16);
+    qreg[s] = __builtin_bit_cast(bf16x8, z);
+  }
+  int tq = 0;
+  if constexpr (BIAS) tq = on ? a.ts_q[qrow] : 0;
+  f32x16 oacc[DV / 32];
+#pragma unroll
+  for (int i = 0; i < DV / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
+
+  // Tiles of keys: T in all, of which every pair sees all keys of the first T0.
+  const int T = (sg.k1 - sg.k0 + ST - 1) / ST;
+  const int T0 = sg.lim0 >= sg.k1 ? T : (sg.lim0 > sg.k0 ? (sg.lim0 - sg.k0) / ST : 0);
+  PageIds ids;
+  const int entries = (sg.k1 + (1 << a.c.ps_log2) - 1) >> a.c.ps_log2;
+  auto copy_k = [&](int t, int buf) __attribute__((always_inline)) {
+    const int key = sg.k0 + t * ST, last = key + ST - 1 < sg.k1 ? key + ST - 1 : sg.k1 - 1;
+    // (V's copies are up to a tile behind K's: a refill starts there)
+    if (!ids.holds(last >> a.c.ps_log2)) ids.fill(a.c, sg.b, (key - ST > sg.k0 ? key - ST : sg.k0) >> a.c.ps_log2, entries);
+    page_copy_async<DQK>(kbuf(buf), a.c.k, a.c.k_page, a.c, ids, sg.h, key, sg.k1, wave, lane);
+    if constexpr (BIAS)
+      if (wave == 0) stamp_copy_async(tbuf(buf), a.c, ids, key, sg.k1, lane);
+  };
+  auto copy_v = [&](int t, int buf) __attribute__((always_inline)) {
+    page_copy_async<DV>(vbuf(buf), a.c.v, a.c.v_page, a.c, ids, sg.h, sg.k0 + t * ST, sg.k1, wave, lane);
+  };
+  auto init_of = [&](int buf, int blk) __attribute__((always_inline)) {
+    return PagedInit<BIAS>{tbuf(buf) + blk * 32, wtab, tq, a.nb, a.f, hh};
+  };
+
+  if (T > 0) {
+    ids.fill(a.c, sg.b, sg.k0 >> a.c.ps_log2, entries);
+    copy_k(0, 0);
+    copy_v(0, 0);
+    if (T > 1 && T0 > 0) copy_k(1, 1);
+  }
+  tile_copy_wait<0>();
+  if constexpr (BIAS) __syncthreads();  // (the table)
+  tile_barrier();
+
+  // The pipelined loop (see hstu_fwd_bf16): iteration j does the steps 2j+1 and 2j+2, step i S(i+1), P(i) and P(i-1) V(i-1).
+  if (T0 > 0) {
+    f32x16 sacc[2];   // S of the blocks of even / odd index
+    bf16x8 pb[2][2];  // P (two 16-key halves) of the blocks of even / odd index
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[x][r] = 0.f;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pb[x][y][e] = (__bf16)0.f;
     }
-    int tq = 0;
-    if constexpr (BIAS) tq = on ? a.ts_q[qrow] : 0;
-    const bool wave_on = wave * 32 < sg.pairs;
-
-    f32x16 oacc[DV / 32];
+    const auto none = [] { return VisBefore{0, 0}; };  // (no block is masked here)
+    if (wave_on) {
+      init_of(0, 0)(sacc[0]);
 #pragma unroll
-    for (int i = 0; i < DV / 32; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
-
-    // Tiles of keys: T in all, of which every pair sees all keys of the first T0.
-    const int T = (sg.k1 - sg.k0 + ST - 1) / ST;
-    const int T0 = sg.lim0 >= sg.k1 ? T : (sg.lim0 > sg.k0 ? (sg.lim0 - sg.k0) / ST : 0);
-    PageIds ids;
-    const int entries = (sg.k1 + (1 << a.c.ps_log2) - 1) >> a.c.ps_log2;
-    auto copy_k = [&](int t, int buf) __attribute__((always_inline)) {
-      const int key = sg.k0 + t * ST, last = key + ST - 1 < sg.k1 ? key + ST - 1 : sg.k1 - 1;
-      // (V's copies are up to a tile behind K's: a refill starts there)
-      if (!ids.holds(last >> a.c.ps_log2)) ids.fill(a.c, pl.b, (key - ST > sg.k0 ? key - ST : sg.k0) >> a.c.ps_log2, entries);
-      page_copy_async<DQK>(kbuf(buf), a.c.k, a.c.k_page, a.c, ids, pl.h, key, sg.k1, wave, lane);
-      if constexpr (BIAS)
-        if (wave == 0) stamp_copy_async(tbuf(buf), a.c, ids, key, sg.k1, lane);
-    };
-    auto copy_v = [&](int t, int buf) __attribute__((always_inline)) {
-      page_copy_async<DV>(vbuf(buf), a.c.v, a.c.v_page, a.c, ids, pl.h, sg.k0 + t * ST, sg.k1, wave, lane);
-    };
-    auto init_of = [&](int buf, int blk) __attribute__((always_inline)) {
-      return PagedInit<BIAS>{tbuf(buf) + blk * 32, wtab, tq, a.nb, a.f, hh};
-    };
-
-    tile_barrier();  // (the last tile's readers are done)
-    if (T > 0) {
-      ids.fill(a.c, pl.b, sg.k0 >> a.c.ps_log2, entries);
-      copy_k(0, 0);
-      copy_v(0, 0);
-      if (T > 1 && T0 > 0) copy_k(1, 1);
+      for (int ks = 0; ks < DQK / 16; ++ks) sacc[0] = mfma(ra.read(kbuf(0), 0, ks), qreg[ks], sacc[0]);
+      fwd_step<DQK, DV, false>(init_of(0, 1), kbuf(0), 1, vbuf(0), 0, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0], oacc,
+                               c1, false, none);
     }
-    tile_copy_wait<0>();
-    if constexpr (BIAS) __syncthreads();  // (the table)
     tile_barrier();
-
-    // The pipelined loop (see hstu_fwd_bf16): iteration j does the steps 2j+1 and 2j+2, step i S(i+1), P(i) and P(i-1) V(i-1).
-    if (T0 > 0) {
-      f32x16 sacc[2];   // S of the blocks of even / odd index
-      bf16x8 pb[2][2];  // P (two 16-key halves) of the blocks of even / odd index
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[x][r] = 0.f;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pb[x][y][e] = (__bf16)0.f;
-      }
-      const auto none = [] { return VisBefore{0, 0}; };  // (no block is masked here)
+    auto iter = [&](int j, auto buf_tag) __attribute__((always_inline)) {
+      constexpr int B0 = decltype(buf_tag)::value, B1 = B0 ^ 1;
+      if (j + 2 <= T0 && j + 2 < T) copy_k(j + 2, B0);
+      if (j + 1 < T) copy_v(j + 1, B1);
       if (wave_on) {
-        init_of(0, 0)(sacc[0]);
-#pragma unroll
-        for (int ks = 0; ks < DQK / 16; ++ks) sacc[0] = mfma(ra.read(kbuf(0), 0, ks), qreg[ks], sacc[0]);
-        fwd_step<DQK, DV, false>(init_of(0, 1), kbuf(0), 1, vbuf(0), 0, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0], oacc,
-                                 c1, false, none);
-      }
-      tile_barrier();
-      auto iter = [&](int j, auto buf_tag) __attribute__((always_inline)) {
-        constexpr int B0 = decltype(buf_tag)::value, B1 = B0 ^ 1;
-        if (j + 2 <= T0 && j + 2 < T) copy_k(j + 2, B0);
-        if (j + 1 < T) copy_v(j + 1, B1);
-        if (wave_on) {
-          fwd_step<DQK, DV, true>(init_of(B1, 0), kbuf(B1), 0, vbuf(B0), 0, ra, ca, qreg, sacc[1], sacc[0], pb[0], pb[1], oacc,
-                                  c1, false, none);
-          if (j + 1 < T0)
-            fwd_step<DQK, DV, true>(init_of(B1, 1), kbuf(B1), 1, vbuf(B0), 1, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0],
-                                    oacc, c1, false, none);
-          else  // P V of the last block
-#pragma unroll
-            for (int c = 0; c < DV / 32; ++c) {
-              oacc[c] = mfma(ca.read(vbuf(B0), 2, c), pb[1][0], oacc[c]);
-              oacc[c] = mfma(ca.read(vbuf(B0), 3, c), pb[1][1], oacc[c]);
-            }
-        }
-        tile_copy_wait<0>();
-        tile_barrier();
-      };
-      for (int j = 0; j < T0; j += 2) {
-        iter(j, std::integral_constant<int, 0>{});
-        if (j + 1 < T0) iter(j + 1, std::integral_constant<int, 1>{});
-      }
-    }
-
-    // Tiles that the diagonal crosses, a block at a time (one or two per tile of pairs: the copies are waited for, in
-    // exchange for a single loop over both buffers).  Tile t's K and V are in the buffers t % 2.
-    // Keys that the lane's pair and the wave's last pair see:
-    int lim = pl.s.n, lim1 = pl.s.n;
-    if (a.causal) {
-      asm volatile("" : "+v"(ln));
-      const int p0 = pl.t * MANY_PAIRS + wave * 32, most = sg.pairs - wave * 32;
-      const int64_t past = (int64_t)pl.s.n - pl.s.m + 1;
-      lim = clampi(past + (p0 + (ln & 31)) / a.group, 0, pl.s.n);
-      lim1 = uniform32(clampi(past + (p0 + (most > 32 ? 32 : (most > 1 ? most : 1)) - 1) / a.group, 0, pl.s.n));
-    }
-    for (int t = T0; t < T; ++t) {
-      const int B = t & 1;
-      int hl = hh;
-      asm volatile("" : "+v"(hl));  // (as above)
-      if (t + 1 < T) {
-        copy_k(t + 1, B ^ 1);
-        copy_v(t + 1, B ^ 1);
-      }
-#pragma unroll 1
-      for (int blk = 0; blk < 2; ++blk) {
-        const int key = sg.k0 + t * ST + blk * 32;
-        if (!wave_on || key >= lim1 || key >= sg.k1) break;
-        f32x16 s;
-        init_of(B, blk)(s);
-#pragma unroll
-        for (int ks = 0; ks < DQK / 16; ++ks) {
-          s = mfma(ra.read(kbuf(B), blk, ks), qreg[ks], s);
-          if (ks & 1) __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
-        }
-        float p[16];
-        const VisBefore vis(lim - 1 - key, hl);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = vis(r) ? s[r] * sigmoid_scaled(s[r], c1) : 0.f;
-        const bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
-        // Rows of V that some pairs of the wave see and others do not: an infinity or NaN there times a zero of P would reach
-        // the pairs that do not see it.  So the product takes the rows before the first such one alone ...
-        int first = 32;  // (rows of the block; a lane's operand holds four runs of four of them)
-#pragma unroll
-        for (int y = 1; y >= 0; --y) {
-          uint32_t lo = 0, hi = 0;  // exponents of all ones in rows 16 y + 4 hl + 0..3 and in rows 16 y + 8 + 4 hl + 0..3
+        fwd_step<DQK, DV, true>(init_of(B1, 0), kbuf(B1), 0, vbuf(B0), 0, ra, ca, qreg, sacc[1], sacc[0], pb[0], pb[1], oacc,
+                                c1, false, none);
+        if (j + 1 < T0)
+          fwd_step<DQK, DV, true>(init_of(B1, 1), kbuf(B1), 1, vbuf(B0), 1, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0],
+                                  oacc, c1, false, none);
+        else  // P V of the last block
 #pragma unroll
           for (int c = 0; c < DV / 32; ++c) {
-            const u32x4 v = __builtin_bit_cast(u32x4, ca.read(vbuf(B), blk * 2 + y, c));
-            const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t bits = (uint32_t)((w[e] & 0x7f80u) == 0x7f80u) | (uint32_t)((w[e] & 0x7f800000u) == 0x7f800000u) << 1;
-              if (e < 2) lo |= bits << (2 * e); else hi |= bits << (2 * e - 4);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            oacc[c] = mfma(ca.read(vbuf(B0), 2, c), pb[1][0], oacc[c]);
+            oacc[c] = mfma(ca.read(vbuf(B0), 3, c), pb[1][1], oacc[c]);
           }
-          const int at_hi = hi ? 16 * y + 8 + 4 * hl + __builtin_ctz(hi) : 32, at_lo = lo ? 16 * y + 4 * hl + __builtin_ctz(lo) : 32;
-          first = at_hi < first ? at_hi : first;
-          first = at_lo < first ? at_lo : first;
-        }
-        first = wave_min(first);
-        uint32_t keep[8];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int rows = first - 8 * x - 4 * hl, c = rows < 0 ? 0 : (rows < 4 ? rows : 4);
-          keep[2 * x] = c >= 2 ? ~0u : (c == 1 ? 0xffffu : 0u);
-          keep[2 * x + 1] = c >= 4 ? ~0u : (c == 3 ? 0xffffu : 0u);
-        }
-#pragma unroll
-        for (int c = 0; c < DV / 32; ++c)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            u32x4 v = __builtin_bit_cast(u32x4, ca.read(vbuf(B), blk * 2 + y, c));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] &= keep[4 * y + e];
-            oacc[c] = mfma(__builtin_bit_cast(bf16x8, v), y ? p1 : p0, oacc[c]);
-            if (y) __builtin_amdgcn_sched_barrier(0);
-          }
-        // ... and the others are added pair by pair where they are seen.
-#pragma unroll 1
-        for (int k = first; k < 32; ++k) {
-          float dot = 0.f;
-#pragma unroll
-          for (int ks = 0; ks < DQK / 16; ++ks) {
-            const bf16x8 x = *HSTU_LDS(bf16x8, kbuf(B) + lds_off<DQK>(blk * 32 + k, ks * 2 + hl));
-            u32x4 qw = __builtin_bit_cast(u32x4, qreg[ks]);
-            asm volatile("" : "+v"(qw));  // (converted here, not once for the loop: no registers for that)
-            const bf16x8 y = __builtin_bit_cast(bf16x8, qw);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)y[e], dot);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          dot += __shfl_xor(dot, 32);
-          if constexpr (BIAS) dot += wtab[bias_bucket(abs_diff(tq, tbuf(B)[blk * 32 + k]), a.nb, a.f)];
-          if (key + k < lim) {
-            const float x = (float)(__bf16)(dot * sigmoid_scaled(dot, c1));
-#pragma unroll
-            for (int c = 0; c < DV / 32; ++c)
-#pragma unroll
-              for (int q4 = 0; q4 < 4; ++q4) {
-                const bf16x4 v = *HSTU_LDS(bf16x4, vbuf(B) + lds_off<DV>(blk * 32 + k, c * 4 + q4) + 8 * hl);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) oacc[c][4 * q4 + e] = __builtin_fmaf(x, (float)v[e], oacc[c][4 * q4 + e]);
-                __builtin_amdgcn_sched_barrier(0);
-              }
-          }
-        }
       }
       tile_copy_wait<0>();
       tile_barrier();
+    };
+    for (int j = 0; j < T0; j += 2) {
+      iter(j, std::integral_constant<int, 0>{});
+      if (j + 1 < T0) iter(j + 1, std::integral_constant<int, 1>{});
     }
-
-    asm volatile("" : "+v"(ln));
-    const int place = wave * 32 + (ln & 31);
-    if (place < sg.pairs) {
-      const int p = pl.t * MANY_PAIRS + place;
-      const int64_t o = (int64_t)(pl.s.row0 + p / a.group) * a.heads + pl.h * a.group + p % a.group;
-      if (sg.first && sg.last)
-        store_owner_major<DV>(a.o, o * DV, oacc, a.alpha * a.inv_n, ln >> 5, 0, a.out_f32);
-      else
-        store_owner_major<DV>(a.partial, ((2 * w + (sg.first ? 1 : 0)) * MANY_PAIRS + place) * DV, oacc, 1.f, ln >> 5, 0, 1);
-    }
-    cut = cut_tile(a, pl, sg, at, share, w, MANY_PAIRS);
-    at += sg.u1 - sg.u0;
-    line.next(a, pl);
   }
-  if (tid == 0) a.cut[w] = cut;
+
+  // Tiles that the diagonal crosses, a block at a time (one or two per tile of pairs: the copies are waited for, in
+  // exchange for a single loop over both buffers).  Tile t's K and V are in the buffers t % 2.
+  // Keys that the lane's pair and the wave's last pair see:
+  int lim = sg.n, lim1 = sg.n;
+  if (a.causal) {
+    const int p0 = sg.t * MANY_PAIRS + wave * 32, most = sg.pairs - wave * 32;
+    const int64_t past = (int64_t)sg.n - sg.m + 1;
+    lim = clampi(past + row, 0, sg.n);
+    lim1 = uniform32(clampi(past + (p0 + (most > 32 ? 32 : (most > 1 ? most : 1)) - 1) / a.group, 0, sg.n));
+  }
+  for (int t = T0; t < T; ++t) {
+    const int B = t & 1;
+    int hl = hh;
+    asm volatile("" : "+v"(hl));  // (as above)
+    if (t + 1 < T) {
+      copy_k(t + 1, B ^ 1);
+      copy_v(t + 1, B ^ 1);
+    }
+#pragma unroll 1
+    for (int blk = 0; blk < 2; ++blk) {
+      const int key = sg.k0 + t * ST + blk * 32;
+      if (!wave_on || key >= lim1 || key >= sg.k1) break;
+      f32x16 s;
+      init_of(B, blk)(s);
+#pragma unroll
+      for (int ks = 0; ks < DQK / 16; ++ks) {
+        s = mfma(ra.read(kbuf(B), blk, ks), qreg[ks], s);
+        if (ks & 1) __builtin_amdgcn_sched_barrier(0);  // (few registers are left)
+      }
+      float p[16];
+      const VisBefore vis(lim - 1 - key, hl);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = vis(r) ? s[r] * sigmoid_scaled(s[r], c1) : 0.f;
+      const bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
+      // Rows of V that some pairs of the wave see and others do not: an infinity or NaN there times a zero of P would reach
+      // the pairs that do not see it.  So the product takes the rows before the first such one alone ...
+      int first = 32;  // (rows of the block; a lane's operand holds four runs of four of them)
+#pragma unroll
+      for (int y = 1; y >= 0; --y) {
+        uint32_t lo = 0, hi = 0;  // exponents of all ones in rows 16 y + 4 hl + 0..3 and in rows 16 y + 8 + 4 hl + 0..3
+#pragma unroll
+        for (int c = 0; c < DV / 32; ++c) {
+          const u32x4 v = __builtin_bit_cast(u32x4, ca.read(vbuf(B), blk * 2 + y, c));
+          const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = (uint32_t)((w[e] & 0x7f80u) == 0x7f80u) | (uint32_t)((w[e] & 0x7f800000u) == 0x7f800000u) << 1;
+            if (e < 2) lo |= bits << (2 * e); else hi |= bits << (2 * e - 4);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const int at_hi = hi ? 16 * y + 8 + 4 * hl + __builtin_ctz(hi) : 32, at_lo = lo ? 16 * y + 4 * hl + __builtin_ctz(lo) : 32;
+        first = at_hi < first ? at_hi : first;
+        first = at_lo < first ? at_lo : first;
+      }
+      first = wave_min(first);
+      uint32_t keep[8];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int rows = first - 8 * x - 4 * hl, c = rows < 0 ? 0 : (rows < 4 ? rows : 4);
+        keep[2 * x] = c >= 2 ? ~0u : (c == 1 ? 0xffffu : 0u);
+        keep[2 * x + 1] = c >= 4 ? ~0u : (c == 3 ? 0xffffu : 0u);
+      }
+#pragma unroll
+      for (int c = 0; c < DV / 32; ++c)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          u32x4 v = __builtin_bit_cast(u32x4, ca.read(vbuf(B), blk * 2 + y, c));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] &= keep[4 * y + e];
+          oacc[c] = mfma(__builtin_bit_cast(bf16x8, v), y ? p1 : p0, oacc[c]);
+          if (y) __builtin_amdgcn_sched_barrier(0);
+        }
+      // ... and the others are added pair by pair where they are seen.
+#pragma unroll 1
+      for (int k = first; k < 32; ++k) {
+        float dot = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < DQK / 16; ++ks) {
+          const bf16x8 x = *HSTU_LDS(bf16x8, kbuf(B) + lds_off<DQK>(blk * 32 + k, ks * 2 + hl));
+          u32x4 qw = __builtin_bit_cast(u32x4, qreg[ks]);
+          asm volatile("" : "+v"(qw));  // (converted here, not once for the loop: no registers for that)
+          const bf16x8 y = __builtin_bit_cast(bf16x8, qw);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)y[e], dot);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        dot += __shfl_xor(dot, 32);
+        if constexpr (BIAS) dot += wtab[bias_bucket(abs_diff(tq, tbuf(B)[blk * 32 + k]), a.nb, a.f)];
+        if (key + k < lim) {
+          const float x = (float)(__bf16)(dot * sigmoid_scaled(dot, c1));
+#pragma unroll
+          for (int c = 0; c < DV / 32; ++c)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              const bf16x4 v = *HSTU_LDS(bf16x4, vbuf(B) + lds_off<DV>(blk * 32 + k, c * 4 + q4) + 8 * hl);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[c][4 * q4 + e] = __builtin_fmaf(x, (float)v[e], oacc[c][4 * q4 + e]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+      }
+    }
+    tile_copy_wait<0>();
+    tile_barrier();
+  }
+
+  if (on) {
+    if (sg.parts == 1)
+      store_owner_major<DV>(a.o, (qrow * a.heads + head) * DV, oacc, a.alpha * a.inv_n, hh, 0, a.out_f32);
+    else
+      store_owner_major<DV>(a.partial, ((int64_t)sg.slot * MANY_PAIRS + slot) * DV, oacc, 1.f, hh, 0, 1);
+  }
 }
 
 template <int DQK, int DV>
 hipError_t launch_many(const PagedArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.workers), block(MANY_WAVES * 64);
+  const dim3 grid((unsigned)a.grid), block(MANY_WAVES * 64);
   if (a.ts_w) hipLaunchKernelGGL((paged_many_kernel<DQK, DV, true>), grid, block, 0, stream, a);
   else hipLaunchKernelGGL((paged_many_kernel<DQK, DV, false>), grid, block, 0, stream, a);
   return hipGetLastError();

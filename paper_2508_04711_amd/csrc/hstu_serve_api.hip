@@ -85,7 +85,7 @@ PagedView view_of(const hstu_paged_cache* c) {
 // How the attention's work is divided (see hstu_paged.h).
 struct Division {
   bool many;
-  int whole, workers, min_share;
+  int whole, workers, grid, min_share;
   size_t front, bytes;  // records of cut tiles; these and partial results
 };
 constexpr int MANY_MEAN = 24;       // pairs per sequence and key/value head from which on the matrix cores bound the pass
@@ -107,15 +107,23 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
   const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap, all = tiles * c->num_kv_heads;
-  d->whole = d->many ? 0 : (keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
+  d->whole = d->many ? keys <= MANY_SHARE : (keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
+  if (d->many) {
+    // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)
+    if (all >= (1ll << 30)) return false;
+    d->workers = MANY_WORKERS;
+    d->grid = (int)((all + 2 * MANY_WORKERS + 7) / 8 * 8);
+    d->front = align_up((size_t)MANY_WORKERS * sizeof(CutTile), 256);
+    d->bytes = d->whole ? 0 : d->front + (size_t)(2 * MANY_WORKERS) * qt * c->d_v * sizeof(float);
+    return true;
+  }
   int64_t workers = all;
   if (!d->whole) {
-    const double most = (double)all * (double)(keys + 2 * TILE_KEYS) / d->min_share + 1.0;
-    const int limit = d->many ? MANY_WORKERS : FEW_WORKERS;
-    workers = most < limit ? (int64_t)most : limit;
+    const double most = (double)all * (double)(keys + 2 * TILE_KEYS) / MIN_SHARE + 1.0;
+    workers = most < FEW_WORKERS ? (int64_t)most : FEW_WORKERS;
   }
-  d->workers = (int)((workers + 7) / 8 * 8);
+  d->workers = d->grid = (int)((workers + 7) / 8 * 8);
   d->front = d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256);
   d->bytes = d->whole ? 0 : d->front + (size_t)d->workers * 2 * (size_t)qt * c->d_v * sizeof(float);
   return true;
@@ -250,7 +258,8 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
   a.causal = params->causal ? 1 : 0;
   a.out_f32 = params->out_dtype == HSTU_F32;
   a.alpha = params->alpha; a.inv_n = 1.f / (float)params->max_len;
-  a.workers = d.workers; a.whole = d.whole; a.min_share = d.min_share;
+  a.workers = d.workers; a.grid = d.grid; a.whole = d.whole; a.min_share = d.min_share;
+  a.records = d.many && !d.whole ? d.workers : 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   {
     TimedLaunch timed(16, stream);
