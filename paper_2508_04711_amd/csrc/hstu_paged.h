@@ -473,11 +473,11 @@ __device__ __forceinline__ CutTile cut_tile(const PagedArgs& a, const Place& p, 
   return c;
 }
 
-// Rows of the 16 from `key` on that lie before `end`, none without a page.  (In a scalar register: the clamp is a vector
+// Rows of the `most` from `key` on that lie before `end`, none without a page.  (In a scalar register: the clamp is a vector
 // instruction, and a descriptor made of its result would be a loop over the lanes.)
-__device__ __forceinline__ int rows_before(int id, int key, int end) {
+__device__ __forceinline__ int rows_before(int id, int key, int end, int most) {
   const int left = end - key;
-  return uniform32(id < 0 || left < 0 ? 0 : (left < 16 ? left : 16));
+  return uniform32(id < 0 || left < 0 ? 0 : (left < most ? left : most));
 }
 
 // Page ids of a sequence, 64 at a time in the lanes of a register: ids outside the cache become -1 (such a page's rows count as

@@ -72,7 +72,7 @@ __device__ __forceinline__ Rows16 rows16(const PagedView& c, const PageIds& ids,
   r.k = c.k + page * c.k_page + row * ROW_K;
   r.v = c.v + page * c.v_page + row * ROW_V;
   r.ts = c.ts + (page << c.ps_log2) + slot;
-  r.n = rows_before(id, key, end);
+  r.n = rows_before(id, key, end, 16);
   return r;
 }
 

@@ -18,6 +18,15 @@ namespace {
 
 constexpr int MANY_WAVES = 4;
 
+// Descriptor of the rows [key, key + most) of one page, those before `end` and none of a page that does not exist.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const char* base, int64_t page_bytes, int row_bytes, const PagedView& c,
+                                                            const PageIds& ids, int h, int key, int end, int most) {
+  const int id = ids.get(key >> c.ps_log2);
+  const int64_t at = ((int64_t)h << c.ps_log2) + (key & ((1 << c.ps_log2) - 1)), page = id < 0 ? 0 : id;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(base + page * page_bytes + at * row_bytes), 0, rows_before(id, key, end, most) * row_bytes,
+                                           0x00020000);
+}
+
 // Copies the wave's share of keys [key, key + 64) into an LDS tile (swizzled like tile_copy_async); rows from `end` on
 // and rows without a page become zeros.  base: K or V pages; ids holds the tile's entries.
 template <int D>
@@ -27,14 +36,19 @@ __device__ __forceinline__ void page_copy_async(char* tile, const char* base, in
   static_assert(RPL <= 16 && LOADS % MANY_WAVES == 0, "a copy stays inside 16 rows; every wave does as many");
   static_assert(MANY_WAVES * RPL % 16 == 0, "the lane's place in its 16 rows is the same in all of them");
   const int row = ((wave * RPL) & 15) + lane / CPR, voff = row * RB + (((lane % CPR) ^ swz<D>(row)) << 4);
+  if (c.ps_log2 >= 6) {  // the tile is in one page (its first key is a multiple of 64): one descriptor for all of it
+    const __amdgpu_buffer_rsrc_t rsrc = page_rsrc(base, page_bytes, RB, c, ids, h, key, end, ST);
+#pragma unroll
+    for (int i = 0; i < LOADS / MANY_WAVES; ++i) {
+      const int idx = i * MANY_WAVES + wave;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, ((idx * RPL) & ~15) * RB, 0, 0);
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < LOADS / MANY_WAVES; ++i) {
-    const int idx = i * MANY_WAVES + wave, row0 = idx * RPL, k16 = key + (row0 & ~15);
-    const int id = ids.get(k16 >> c.ps_log2);
-    const int64_t at = ((int64_t)h << c.ps_log2) + (k16 & ((1 << c.ps_log2) - 1)), page = id < 0 ? 0 : id;
-    const int rows = rows_before(id, k16, end);
-    const __amdgpu_buffer_rsrc_t rsrc =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(base + page * page_bytes + at * RB), 0, rows * RB, 0x00020000);
+    const int idx = i * MANY_WAVES + wave;
+    const __amdgpu_buffer_rsrc_t rsrc = page_rsrc(base, page_bytes, RB, c, ids, h, key + ((idx * RPL) & ~15), end, 16);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, 0, 0, 0);
   }
 }
@@ -43,7 +57,7 @@ __device__ __forceinline__ void page_copy_async(char* tile, const char* base, in
 __device__ __forceinline__ void stamp_copy_async(int* tile, const PagedView& c, const PageIds& ids, int key, int end, int lane) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int k16 = key + 16 * i, id = ids.get(k16 >> c.ps_log2), rows = rows_before(id, k16, end);
+    const int k16 = key + 16 * i, id = ids.get(k16 >> c.ps_log2), rows = rows_before(id, k16, end, 16);
     const int32_t* p = c.ts + ((int64_t)(id < 0 ? 0 : id) << c.ps_log2) + (k16 & ((1 << c.ps_log2) - 1));
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows * 4, 0x00020000);
     if (lane >> 4 == i) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile), 4, (lane & 15) * 4, 0, 0, 0);
@@ -167,13 +181,18 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
 #pragma unroll
         for (int e = 0; e < 8; ++e) pb[x][y][e] = (__bf16)0.f;
     }
-    const auto none = [] { return VisBefore{0, 0}; };  // (no block is masked here)
+    // No block is masked here, but the compiler must not know: without the step's branch it moves the SiLU's vector instructions
+    // behind the matrix instructions that they are to run beside (burst 165 us, MFMA_BEFORE).
+    int never = 0;
+    asm volatile("" : "+s"(never));
+    const bool mask = never != 0;
+    const auto none = [&] { return VisBefore{never, hh}; };
     if (wave_on) {
       init_of(0, 0)(sacc[0]);
 #pragma unroll
       for (int ks = 0; ks < DQK / 16; ++ks) sacc[0] = mfma(ra.read(kbuf(0), 0, ks), qreg[ks], sacc[0]);
       fwd_step<DQK, DV, false>(init_of(0, 1), kbuf(0), 1, vbuf(0), 0, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0], oacc,
-                               c1, false, none);
+                               c1, mask, none);
     }
     tile_barrier();
     auto iter = [&](int j, auto buf_tag) __attribute__((always_inline)) {
@@ -182,16 +201,10 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
       if (j + 1 < T) copy_v(j + 1, B1);
       if (wave_on) {
         fwd_step<DQK, DV, true>(init_of(B1, 0), kbuf(B1), 0, vbuf(B0), 0, ra, ca, qreg, sacc[1], sacc[0], pb[0], pb[1], oacc,
-                                c1, false, none);
+                                c1, mask, none);
         if (j + 1 < T0)
           fwd_step<DQK, DV, true>(init_of(B1, 1), kbuf(B1), 1, vbuf(B0), 1, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0],
-                                  oacc, c1, false, none);
-        else  // P V of the last block
-#pragma unroll
-          for (int c = 0; c < DV / 32; ++c) {
-            oacc[c] = mfma(ca.read(vbuf(B0), 2, c), pb[1][0], oacc[c]);
-            oacc[c] = mfma(ca.read(vbuf(B0), 3, c), pb[1][1], oacc[c]);
-          }
+                                  oacc, c1, mask, none);
       }
       tile_copy_wait<0>();
       tile_barrier();
@@ -200,6 +213,15 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
       iter(j, std::integral_constant<int, 0>{});
       if (j + 1 < T0) iter(j + 1, std::integral_constant<int, 1>{});
     }
+    if (wave_on) {  // P V of the last block
+      const char* vt = vbuf((T0 - 1) & 1);
+#pragma unroll
+      for (int c = 0; c < DV / 32; ++c) {
+        oacc[c] = mfma(ca.read(vt, 2, c), pb[1][0], oacc[c]);
+        oacc[c] = mfma(ca.read(vt, 3, c), pb[1][1], oacc[c]);
+      }
+    }
+    tile_barrier();  // (the next copies go where these values were read)
   }
 
   // Tiles that the diagonal crosses, a block at a time (one or two per tile of pairs: the copies are waited for, in
