@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -205,18 +206,18 @@ def load_library():
     lib.hstu_debug_dq_atomic_rate.restype = ctypes.c_int
     lib.hstu_debug_dq_atomic_rate.argtypes = [vp, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                               ctypes.POINTER(ctypes.c_double), vp]
-    rp, cp = ctypes.POINTER(_RotaryDesc), ctypes.POINTER(_PagedCache)
+    # (structures as void pointers: an address, a ctypes object by reference, or packed bytes)
     lib.hstu_rotary.restype = ctypes.c_int
-    lib.hstu_rotary.argtypes = [rp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                ctypes.POINTER(_RotaryTensor), vp, i32p, vp]
+    lib.hstu_rotary.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                vp, vp, i32p, vp]
     lib.hstu_cache_append.restype = ctypes.c_int
-    lib.hstu_cache_append.argtypes = [cp, rp, ctypes.c_int64, ctypes.POINTER(_RotaryTensor), vp, ctypes.c_int64, vp,
+    lib.hstu_cache_append.argtypes = [vp, vp, ctypes.c_int64, vp, vp, ctypes.c_int64, vp,
                                       ctypes.c_int64, vp, i32p, vp]
     lib.hstu_paged_attn_fwd.restype = ctypes.c_int
-    lib.hstu_paged_attn_fwd.argtypes = [ctypes.POINTER(_PagedParams), cp, bp, vp, ctypes.c_int64, i32p, vp, vp,
+    lib.hstu_paged_attn_fwd.argtypes = [vp, vp, vp, vp, ctypes.c_int64, i32p, vp, vp,
                                         ctypes.c_size_t, vp]
     lib.hstu_paged_attn_workspace_bytes.restype = ctypes.c_size_t
-    lib.hstu_paged_attn_workspace_bytes.argtypes = [ctypes.POINTER(_PagedParams), cp]
+    lib.hstu_paged_attn_workspace_bytes.argtypes = [vp, vp]
     lib.hstu_schedule_tile_rows.restype = ctypes.c_int
     lib.hstu_schedule_tile_rows.argtypes = [pp, ctypes.c_int]
     _lib = lib
@@ -915,93 +916,109 @@ def hstu_rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str
     return torch.from_numpy(f).to(torch.device("cuda") if device is None else device)
 
 
-def _check_rows(t: torch.Tensor, name: str, device, dtype=None) -> None:
-    """[rows, heads, dim] of one device whose rows are contiguous (a slice of a wider projection is one)."""
-    if t.dim() != 3 or not t.is_cuda:
-        raise ValueError("%s must be a device tensor [rows, heads, dim]" % name)
-    if t.device != device:
-        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
-    if dtype is not None and t.dtype != dtype:
+# Structures of the C ABI as packed bytes, which ctypes hands over as they are (a ctypes structure costs a microsecond each).
+_ROTARY_DESC = struct.Struct("=QiifI")       # hstu_rotary_desc
+_ROTARY_TENSOR = struct.Struct("=QQqqii")    # hstu_rotary_tensor
+_PAGED_PARAMS = struct.Struct("=iifiiiq")    # hstu_paged_attn_params
+_CODES = {torch.bfloat16: HSTU_BF16, torch.float32: HSTU_F32}
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+class _Elsewhere:
+    """The device and the stream of a call as torch's current ones, so that what the call allocates belongs to that stream (see
+    _allocates_on_its_stream)."""
+
+    def __init__(self, index: int, stream):
+        if stream is not None and stream.device.index != index:
+            raise ValueError("stream is of %s, the tensors are on cuda:%d" % (stream.device, index))
+        self.device, self.stream = torch.cuda.device(index), torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self.device.__enter__()
+        self.stream.__enter__()
+
+    def __exit__(self, *exc):
+        self.stream.__exit__(*exc)
+        self.device.__exit__(*exc)
+
+
+def _rows(t: torch.Tensor, name: str, index: int, dtype):
+    """(rows, heads, dim, row stride) of a tensor [rows, heads, dim] on device `index` whose rows are contiguous: a slice of a wider
+    projection is one."""
+    if t.get_device() != index or index < 0:
+        raise ValueError("%s must be a tensor on the device of the call" % name)
+    if t.dtype is not dtype:
         raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if not t.is_contiguous() and ((t.shape[2] > 1 and t.stride(2) != 1)
-                                  or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError("%s must be [rows, heads, dim]" % name)
+    rows, heads, dim = shape
+    if t.is_contiguous():
+        return rows, heads, dim, heads * dim
+    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
         raise ValueError("%s: a row's heads must be contiguous" % name)
+    return rows, heads, dim, t.stride(0) if rows > 1 else heads * dim
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    # (the stride of a single row says nothing)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-
-
-def _check_index(t: torch.Tensor, name: str, device, size: Optional[int] = None) -> None:
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or not t.is_contiguous() \
+def _index(t: torch.Tensor, name: str, index: int, size: Optional[int] = None) -> int:
+    """Address of a contiguous 1-d int32 tensor."""
+    if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() \
             or (size is not None and t.shape[0] != size):
-        raise ValueError("%s must be a contiguous 1-d int32 tensor on %s%s"
-                         % (name, device, "" if size is None else " with %d entries" % size))
+        raise ValueError("%s must be a contiguous 1-d int32 tensor on the device of the call%s"
+                         % (name, "" if size is None else ", with %d entries" % size))
+    return t.data_ptr()
 
 
-def _rotary_desc(inv_freq: torch.Tensor, interleaved: bool, scale: float, device) -> _RotaryDesc:
-    if inv_freq.dtype != torch.float64 or inv_freq.device != device or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
-        raise ValueError("inv_freq must be a contiguous 1-d fp64 tensor on %s (hstu_rotary_frequencies)" % (device,))
-    return _RotaryDesc(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale, 0)
-
-
-def _on_its_device(fn):
-    """Runs `fn` with the device of its first argument (a tensor, a list of them, a cache) as the current one, and its stream=
-    argument as torch's current stream (see _allocates_on_its_stream)."""
-    @functools.wraps(fn)
-    def wrapped(first, *args, **kwargs):
-        t = first[0] if isinstance(first, (list, tuple)) and len(first) else first
-        device = getattr(t, "device", None)
-        if device is not None and device.type == "cuda" and device.index != torch.cuda.current_device():
-            with torch.cuda.device(device):
-                return wrapped(first, *args, **kwargs)
-        stream = kwargs.get("stream")
-        if stream is None or stream == torch.cuda.current_stream():
-            return fn(first, *args, **kwargs)
-        if device is not None and stream.device != device:
-            raise ValueError("stream is of %s, the tensors are on %s" % (stream.device, device))
-        with torch.cuda.stream(stream):
-            return fn(first, *args, **kwargs)
-    return wrapped
+def _rotary_desc(inv_freq: torch.Tensor, interleaved: bool, scale: float, index: int) -> bytes:
+    if inv_freq.dtype is not torch.float64 or inv_freq.get_device() != index or inv_freq.dim() != 1 \
+            or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous 1-d fp64 tensor on the device of the call (hstu_rotary_frequencies)")
+    return _ROTARY_DESC.pack(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale, 0)
 
 
 def _rotary_call(where, backward, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, stream):
-    tensors = list(tensors)
     n = len(tensors)
     if not 1 <= n <= 4:
         raise ValueError("1 to 4 tensors per call")
     first = tensors[0]
-    device, rows = first.device, first.shape[0]
-    if out is None:
-        out = [torch.empty(t.shape, dtype=t.dtype, device=device) for t in tensors]
-    elif len(out) != n:
+    index, dtype = first.get_device(), first.dtype
+    if stream is not None or (index >= 0 and index != _current_device()):
+        with _Elsewhere(index, stream):
+            return _rotary_call(where, backward, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, None)
+    code = _CODES.get(dtype)
+    if code is None:
+        raise TypeError("unsupported dtype %s" % dtype)
+    if out is not None and len(out) != n:
         raise ValueError("one output per tensor")
-    arr = (_RotaryTensor * n)()
-    for i, (t, o) in enumerate(zip(tensors, out)):
-        _check_rows(t, "tensors[%d]" % i, device, first.dtype)
-        if o is not t:
-            _check_rows(o, "out[%d]" % i, device, first.dtype)
-        if t.shape[0] != rows or o.shape != t.shape:
-            raise ValueError("tensors and outputs must have the same rows, an output its tensor's shape")
-        arr[i] = _RotaryTensor(t.data_ptr(), o.data_ptr(), _row_stride(t), _row_stride(o), t.shape[1], t.shape[2])
+    rows, outs, packed = None, [], []
+    for i, t in enumerate(tensors):
+        r, heads, dim, stride = _rows(t, "tensors[%d]" % i, index, dtype)
+        if rows is None:
+            rows = r
+        if out is None:
+            o, ostride = torch.empty_like(t, memory_format=torch.contiguous_format), heads * dim
+        else:
+            o = out[i]
+            ro, ho, do, ostride = _rows(o, "out[%d]" % i, index, dtype)
+            if (ro, ho, do) != (r, heads, dim):
+                raise ValueError("out[%d] must have its tensor's shape" % i)
+        if r != rows:
+            raise ValueError("tensors must have the same rows")
+        outs.append(o)
+        packed.append(_ROTARY_TENSOR.pack(t.data_ptr(), o.data_ptr(), stride, ostride, heads, dim))
     if (seq_offsets is None) == (positions is None):
         raise ValueError("either seq_offsets or positions")
-    batch = 0
     if positions is not None:
-        _check_index(positions, "positions", device, rows)
+        batch, pos, off = 0, _index(positions, "positions", index, rows), None
     else:
-        _check_index(seq_offsets, "seq_offsets", device)
-        batch = seq_offsets.shape[0] - 1
-    desc = _rotary_desc(inv_freq, interleaved, scale, device)
-    rc = load_library().hstu_rotary(ctypes.byref(desc), backward, _dtype_code(first), batch, rows, n, arr,
-                                    _ptr(positions), _ptr(seq_offsets), _stream(stream))
+        batch, pos, off = seq_offsets.shape[0] - 1, None, _index(seq_offsets, "seq_offsets", index)
+    rc = load_library().hstu_rotary(_rotary_desc(inv_freq, interleaved, scale, index), backward, code, batch, rows, n,
+                                    b"".join(packed), pos, off, _stream(None))
     if rc != 0:
         raise HstuError(rc, where)
-    return out
+    return outs
 
 
-@_on_its_device
 def hstu_rotary_fwd(tensors, inv_freq: torch.Tensor, seq_offsets: Optional[torch.Tensor] = None,
                     positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0,
                     out=None, stream=None):
@@ -1015,7 +1032,6 @@ def hstu_rotary_fwd(tensors, inv_freq: torch.Tensor, seq_offsets: Optional[torch
     return _rotary_call("hstu_rotary_fwd", 0, tensors, inv_freq, seq_offsets, positions, interleaved, scale, out, stream)
 
 
-@_on_its_device
 def hstu_rotary_bwd(tensors, inv_freq: torch.Tensor, seq_offsets: Optional[torch.Tensor] = None,
                     positions: Optional[torch.Tensor] = None, interleaved: bool = False, scale: float = 1.0,
                     out=None, stream=None):
@@ -1049,7 +1065,7 @@ class HstuPagedCache:
         if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.device != device or \
                 (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be an int32 tensor [batch, pages_per_seq] on %s, rows contiguous" % (device,))
-        _check_index(seq_lens, "seq_lens", device, page_table.shape[0])
+        _index(seq_lens, "seq_lens", k_pages.get_device(), page_table.shape[0])
         if ts_pages is not None and (ts_pages.dtype != torch.int32 or ts_pages.device != device
                                      or tuple(ts_pages.shape) != (pages, ps) or not ts_pages.is_contiguous()):
             raise ValueError("ts_pages must be a contiguous int32 tensor [num_pages, page_size] on %s" % (device,))
@@ -1058,14 +1074,16 @@ class HstuPagedCache:
         self.device, self.dtype = device, dtype
         self.batch, self.pages_per_seq = page_table.shape
         self.num_kv_heads, self.page_size, self.d_qk, self.d_v = heads, ps, dqk, dv
+        self._index = k_pages.get_device()
+        self._need = (None, 0)  # workspace of the last call's (heads, rows, max_kv)
         self._struct = _PagedCache(
             self.batch, heads, dqk, dv, ps, self.pages_per_seq, _code(dtype), 0, pages,
             k_pages.stride(0) if pages > 1 else heads * ps * dqk, v_pages.stride(0) if pages > 1 else heads * ps * dv,
             page_table.stride(0) if self.batch > 1 else self.pages_per_seq, k_pages.data_ptr(), v_pages.data_ptr(),
             _ptr(ts_pages), page_table.data_ptr(), seq_lens.data_ptr())
+        self._address = ctypes.addressof(self._struct)
 
 
-@_on_its_device
 def hstu_cache_append(cache: HstuPagedCache, k: torch.Tensor, v: torch.Tensor, seq_offsets: torch.Tensor,
                       q: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
                       interleaved: bool = False, scale: float = 1.0, timestamps: Optional[torch.Tensor] = None,
@@ -1077,86 +1095,99 @@ def hstu_cache_append(cache: HstuPagedCache, k: torch.Tensor, v: torch.Tensor, s
     returns the turned q (q_out, which may be q itself, or a new tensor), None without q.  timestamps: int32 [rows], needed
     iff the cache holds timestamps.
     """
-    device, dtype = cache.device, cache.dtype
-    rows = k.shape[0]
-    _check_rows(k, "k", device, dtype)
-    _check_rows(v, "v", device, dtype)
-    if k.shape[1:] != (cache.num_kv_heads, cache.d_qk) or v.shape != (rows, cache.num_kv_heads, cache.d_v):
-        raise ValueError("k and v must be [rows, %d, %d] and [rows, %d, %d]"
-                         % (cache.num_kv_heads, cache.d_qk, cache.num_kv_heads, cache.d_v))
-    _check_index(seq_offsets, "seq_offsets", device, cache.batch + 1)
+    index, dtype = cache._index, cache.dtype
+    if stream is not None or index != _current_device():
+        with _Elsewhere(index, stream):
+            return hstu_cache_append(cache, k, v, seq_offsets, q, inv_freq, interleaved, scale, timestamps, q_out)
+    rows, kheads, kdim, kstride = _rows(k, "k", index, dtype)
+    vrows, vheads, vdim, vstride = _rows(v, "v", index, dtype)
+    heads = cache.num_kv_heads
+    if (kheads, kdim, vrows, vheads, vdim) != (heads, cache.d_qk, rows, heads, cache.d_v):
+        raise ValueError("k and v must be [rows, %d, %d] and [rows, %d, %d]" % (heads, cache.d_qk, heads, cache.d_v))
+    off = _index(seq_offsets, "seq_offsets", index, cache.batch + 1)
     if (timestamps is None) != (cache.ts_pages is None):
         raise ValueError("timestamps are needed iff the cache holds timestamps")
-    if timestamps is not None:
-        _check_index(timestamps, "timestamps", device, rows)
-    desc = None if inv_freq is None else ctypes.byref(_rotary_desc(inv_freq, interleaved, scale, device))
+    ts = None if timestamps is None else _index(timestamps, "timestamps", index, rows)
+    desc = None if inv_freq is None else _rotary_desc(inv_freq, interleaved, scale, index)
     tensor = None
     if q is not None:
-        _check_rows(q, "q", device, dtype)
-        if q.shape[0] != rows or q.shape[2] != cache.d_qk:
+        qrows, qheads, qdim, qstride = _rows(q, "q", index, dtype)
+        if qrows != rows or qdim != cache.d_qk:
             raise ValueError("q must be [%d, heads, %d]" % (rows, cache.d_qk))
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=device)
+            q_out, ostride = torch.empty_like(q, memory_format=torch.contiguous_format), qheads * qdim
         else:
-            _check_rows(q_out, "q_out", device, dtype)
-            if q_out.shape != q.shape:
+            orows, oheads, odim, ostride = _rows(q_out, "q_out", index, dtype)
+            if (orows, oheads, odim) != (qrows, qheads, qdim):
                 raise ValueError("q_out must have q's shape")
-        tensor = ctypes.byref(_RotaryTensor(q.data_ptr(), q_out.data_ptr(), _row_stride(q), _row_stride(q_out),
-                                            q.shape[1], q.shape[2]))
+        tensor = _ROTARY_TENSOR.pack(q.data_ptr(), q_out.data_ptr(), qstride, ostride, qheads, qdim)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    rc = load_library().hstu_cache_append(ctypes.byref(cache._struct), desc, rows, tensor, k.data_ptr(), _row_stride(k),
-                                          v.data_ptr(), _row_stride(v), _ptr(timestamps), seq_offsets.data_ptr(),
-                                          _stream(stream))
+    rc = load_library().hstu_cache_append(cache._address, desc, rows, tensor, k.data_ptr(), kstride, v.data_ptr(), vstride,
+                                          ts, off, _stream(None))
     if rc != 0:
         raise HstuError(rc, "hstu_cache_append")
     return q_out
 
 
-def _paged_params(heads, max_len, alpha, causal, out_dtype, max_kv, rows) -> _PagedParams:
-    return _PagedParams(heads, max_len, alpha, 1 if causal else 0, _code(out_dtype), 0 if max_kv is None else max_kv, rows)
+def _paged_params(heads, max_len, alpha, causal, code, max_kv, rows) -> bytes:
+    return _PAGED_PARAMS.pack(heads, max_len, alpha, 1 if causal else 0, code, 0 if max_kv is None else max_kv, rows)
 
 
 def hstu_paged_attn_workspace_bytes(cache: HstuPagedCache, num_heads: int, new_rows: int,
                                     max_kv: Optional[int] = None) -> int:
     """Bytes of workspace of an attention call of `new_rows` rows over the cache (0: out of range)."""
-    p = _paged_params(num_heads, 1, 1.0, True, cache.dtype, max_kv, new_rows)
-    return int(load_library().hstu_paged_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(cache._struct)))
+    p = _paged_params(num_heads, 1, 1.0, True, _CODES[cache.dtype], max_kv, new_rows)
+    return int(load_library().hstu_paged_attn_workspace_bytes(p, cache._address))
 
 
-def _paged_call(where, q, cache, seq_offsets, bias, max_len, alpha, causal, max_kv, out, workspace, stream, out_dtype):
-    device = cache.device
-    _check_rows(q, "q", device, cache.dtype)
-    rows, heads, dim = q.shape
+def _paged_call(where, q, cache, seq_offsets, timestamps, ts_weights, groups_log2, max_len, alpha, causal, max_kv, out,
+                workspace, stream, out_dtype):
+    index, dtype = cache._index, cache.dtype
+    if stream is not None or index != _current_device():
+        with _Elsewhere(index, stream):
+            return _paged_call(where, q, cache, seq_offsets, timestamps, ts_weights, groups_log2, max_len, alpha, causal, max_kv,
+                               out, workspace, None, out_dtype)
+    rows, heads, dim, stride = _rows(q, "q", index, dtype)
     if dim != cache.d_qk or heads % cache.num_kv_heads != 0:
         raise ValueError("q must be [rows, a multiple of %d heads, %d]" % (cache.num_kv_heads, cache.d_qk))
-    _check_index(seq_offsets, "seq_offsets", device, cache.batch + 1)
+    off = _index(seq_offsets, "seq_offsets", index, cache.batch + 1)
+    bias = None
+    if timestamps is not None:
+        if cache.ts_pages is None:
+            raise ValueError("the cache holds no timestamps")
+        _index(timestamps, "timestamps", index, rows)
+        if ts_weights.get_device() != index:
+            raise ValueError("ts_weights must be on the device of the call")
+        bias = ctypes.byref(_bias_desc(timestamps, ts_weights, None, groups_log2, rows))
     if out is None:
-        odt = cache.dtype if out_dtype is None else out_dtype
-        if dim == cache.d_v and odt is cache.dtype:
-            out = _empty(q, odt)
-        else:
-            out = torch.empty((rows, heads, cache.d_v), dtype=odt, device=device)
+        odt = dtype if out_dtype is None else out_dtype
+        out = _empty(q, odt) if dim == cache.d_v else torch.empty((rows, heads, cache.d_v), dtype=odt, device=q.device)
     else:
         odt = out.dtype
         _check_tensor(out, "out", rows, heads, cache.d_v, odt)
-        if out.device != device or (out_dtype is not None and out_dtype != odt):
-            raise ValueError("out must be %s on %s" % (out_dtype or odt, device))
+        if out.get_device() != index or (out_dtype is not None and out_dtype != odt):
+            raise ValueError("out must be %s on the device of the call" % (out_dtype or odt))
     lib = load_library()
-    p = ctypes.byref(_paged_params(heads, max_len, alpha, causal, odt, max_kv, rows))
-    c = ctypes.byref(cache._struct)
+    p = _paged_params(heads, max_len, alpha, causal, _code(odt), max_kv, rows)
     if workspace is None:
-        workspace = torch.empty(max(lib.hstu_paged_attn_workspace_bytes(p, c), 256), dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous and on %s" % (device,))
-    rc = lib.hstu_paged_attn_fwd(p, c, bias, q.data_ptr(), _row_stride(q), seq_offsets.data_ptr(), out.data_ptr(),
-                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+        key = (heads, rows, max_kv)
+        if cache._need[0] != key:
+            cache._need = (key, lib.hstu_paged_attn_workspace_bytes(p, cache._address))
+        need = cache._need[1]
+        # (256: the call cuts nothing and touches no workspace)
+        ws, size = (out.data_ptr(), 0) if need <= 256 else (torch.empty(need, dtype=torch.uint8, device=q.device), need)
+    else:
+        if workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous and on the device of the call")
+        ws, size = workspace, workspace.numel() * workspace.element_size()
+    rc = lib.hstu_paged_attn_fwd(p, cache._address, bias, q.data_ptr(), stride, off, out.data_ptr(),
+                                 ws if type(ws) is int else ws.data_ptr(), size, _stream(None))
     if rc != 0:
         raise HstuError(rc, where)
     return out
 
 
-@_on_its_device
 def hstu_paged_attn_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: torch.Tensor, max_len: int, alpha: float,
                         causal: bool = True, max_kv: Optional[int] = None, out: Optional[torch.Tensor] = None,
                         workspace: Optional[torch.Tensor] = None, stream=None,
@@ -1168,11 +1199,10 @@ def hstu_paged_attn_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: tor
     heads may be a multiple of the cache's.  max_kv: a bound on cache.seq_lens that the caller knows (a hint for the
     division of the work; nothing is left out beyond it).
     """
-    return _paged_call("hstu_paged_attn_fwd", q, cache, seq_offsets, None, max_len, alpha, causal, max_kv, out, workspace,
-                       stream, out_dtype)
+    return _paged_call("hstu_paged_attn_fwd", q, cache, seq_offsets, None, None, 0, max_len, alpha, causal, max_kv, out,
+                       workspace, stream, out_dtype)
 
 
-@_on_its_device
 def hstu_paged_attn_bias_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: torch.Tensor, timestamps: torch.Tensor,
                              ts_weights: torch.Tensor, groups_log2: int, max_len: int, alpha: float, causal: bool = True,
                              max_kv: Optional[int] = None, out: Optional[torch.Tensor] = None,
@@ -1180,10 +1210,7 @@ def hstu_paged_attn_bias_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets
                              out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """hstu_paged_attn_fwd with the timestamp bias of hstu_jagged_attn_bias_fwd: timestamps [rows] of the new rows against
     the cached rows' (cache.ts_pages)."""
-    if cache.ts_pages is None:
-        raise ValueError("the cache holds no timestamps")
-    if q.device != cache.device or timestamps.device != cache.device or ts_weights.device != cache.device:
-        raise ValueError("q, timestamps and ts_weights must be on %s" % (cache.device,))
-    bias = _bias_desc(timestamps, ts_weights, None, groups_log2, q.shape[0])
-    return _paged_call("hstu_paged_attn_bias_fwd", q, cache, seq_offsets, ctypes.byref(bias), max_len, alpha, causal, max_kv,
-                       out, workspace, stream, out_dtype)
+    if timestamps is None or ts_weights is None:
+        raise ValueError("the bias needs timestamps and ts_weights")
+    return _paged_call("hstu_paged_attn_bias_fwd", q, cache, seq_offsets, timestamps, ts_weights, groups_log2, max_len, alpha,
+                       causal, max_kv, out, workspace, stream, out_dtype)
