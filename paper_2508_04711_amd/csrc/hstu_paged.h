@@ -144,12 +144,14 @@ struct Line {
     sum = 0;
     m = n = row0 = 0;
     const int64_t b0 = (int64_t)lane * chunk;
-    for (int i = 0; i < chunk; ++i)
-      if (b0 + i < a.batch) {
-        const SeqWork s = read_work<QT>(a, (int)b0 + i);
-        sum += s.cost;
-        m = s.m; n = s.n; row0 = s.row0;
-      }
+    // (no branch on the sequence: the loads of several are in flight together)
+#pragma unroll 4
+    for (int i = 0; i < chunk; ++i) {
+      const bool in = b0 + i < a.batch;
+      const SeqWork s = read_work<QT>(a, in ? (int)b0 + i : a.batch - 1);
+      sum += in ? s.cost : 0;
+      m = s.m; n = s.n; row0 = s.row0;
+    }
     sum *= a.kv_heads;
     incl = wave_scan64(sum);
     total = lane64(incl, 63);
@@ -345,25 +347,27 @@ struct Units {
     const int64_t b0 = (int64_t)lane * chunk;
     int64_t keys = 0;
     int tiles = 0;
-    for (int i = 0; i < chunk; ++i)
-      if (b0 + i < a.batch) {
-        read(a, (int)b0 + i, m, n, row0);
-        const int t = (int)(((int64_t)m * a.group + QT - 1) / QT);
-        tiles += t;
-        keys += t * (int64_t)n;
-      }
+#pragma unroll 4
+    for (int i = 0; i < chunk; ++i) {
+      const bool in = b0 + i < a.batch;
+      read(a, in ? (int)b0 + i : a.batch - 1, m, n, row0);
+      const int t = in ? (int)(((int64_t)m * a.group + QT - 1) / QT) : 0;
+      tiles += t;
+      keys += t * (int64_t)n;
+    }
     const int all_tiles = __builtin_amdgcn_readlane(wave_scan(tiles), 63) * a.kv_heads;
     const int64_t all = lane64(wave_scan64(keys), 63) * a.kv_heads;
     share = find_share(a, tiles, all_tiles, all);
     lane_units = lane_cut_units = lane_cut_tiles = 0;
-    for (int i = 0; i < chunk; ++i)
-      if (b0 + i < a.batch) {
-        if (chunk > 1) read(a, (int)b0 + i, m, n, row0);
-        const Counts c = counts(a, m, n);
-        lane_units += c.units;
-        lane_cut_units += c.cut_units;
-        lane_cut_tiles += c.cut_tiles;
-      }
+#pragma unroll 4
+    for (int i = 0; i < chunk; ++i) {
+      const bool in = b0 + i < a.batch;
+      if (chunk > 1) read(a, in ? (int)b0 + i : a.batch - 1, m, n, row0);
+      const Counts c = counts(a, in ? m : 0, n);
+      lane_units += c.units;
+      lane_cut_units += c.cut_units;
+      lane_cut_tiles += c.cut_tiles;
+    }
     units = wave_scan(lane_units);
     cut_units = wave_scan(lane_cut_units);
     cut_tiles = wave_scan(lane_cut_tiles);

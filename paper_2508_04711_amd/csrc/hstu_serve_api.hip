@@ -91,11 +91,11 @@ struct Division {
 constexpr int MANY_MEAN = 24;       // pairs per sequence and key/value head from which on the matrix cores bound the pass
 constexpr int MANY_WORKERS = 512;   // two workgroups per CU
 constexpr int MANY_SHARE = 128;
-constexpr int FEW_WORKERS = 2048;   // two one-wave workers per SIMD
+constexpr int FEW_WORKERS = 1024;   // a one-wave worker per SIMD: 768..1536 are within 3 %, 2048 and 512 3 to 5 % behind
 constexpr int MIN_SHARE = 64;       // keys that are worth a worker
-constexpr int WHOLE_KEYS = 128;     // up to that many keys a tile is one worker's, uncut
-constexpr int TEAM_KEYS = 1024;     // ... where the worker is a team of waves
-constexpr int TEAM_TILES = 512;     // and that many tiles
+constexpr int WHOLE_KEYS = 512;     // up to that many keys a tile is one worker's, uncut
+constexpr int TEAM_BYTES = 1 << 19; // up to that many bytes of keys and values a tile, and that many tiles, the worker is a
+constexpr int TEAM_TILES = 512;     // team of waves, which joins its results itself
 
 // false: sizes out of range
 bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division* d) {
@@ -103,11 +103,12 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   const int64_t cap = view_of(c).cap, pairs = p->new_rows * group;
   d->many = c->dtype == HSTU_BF16 && pairs > (int64_t)MANY_MEAN * c->batch;
   const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS;
-  const int64_t tiles = pairs / qt + (c->batch < p->new_rows ? c->batch : p->new_rows);  // (of one head; at most)
+  // tiles of one head, at most: every sequence with rows may leave one of its tiles with a single pair
+  const int64_t tiles = (pairs + (qt - 1) * (c->batch < p->new_rows ? c->batch : p->new_rows)) / qt;
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
   const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap, all = tiles * c->num_kv_heads;
-  d->whole = d->many ? keys <= MANY_SHARE : (keys <= TEAM_KEYS && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
+  d->whole = d->many ? keys <= MANY_SHARE : (keys * (c->d_qk + c->d_v) * size_of(c->dtype) <= TEAM_BYTES && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
   if (d->many) {
     // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)

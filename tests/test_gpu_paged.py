@@ -157,6 +157,33 @@ def test_long_histories_are_cut_and_joined(dtype):
     assert e.value.status == -4
 
 
+@pytest.mark.parametrize("heads,kv_heads,ps", [(2, 1, 16), (3, 3, 32), (1, 1, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_over_long_histories(heads, kv_heads, ps, causal):
+    """Tiles of 128 pairs cut into pieces, some of which no row of a tile sees; histories shorter than their new rows."""
+    pr = Problem("bf16", [2500, 700, 3, 0, 1333], [300, 130, 7, 0, 257] if causal else [300, 1, 7, 2, 60], heads, kv_heads, 32, 32,
+                 ps, seed=ps, fill=NAN if causal else 0.0)
+    got = pr.call(causal=causal)
+    pr.check(got, causal)
+    assert torch.equal(got, pr.call(causal=causal))
+    ws = torch.empty(hstu.hstu_paged_attn_workspace_bytes(pr.cache(), heads, pr.rows), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xff)
+    assert torch.equal(pr.call(causal=causal, workspace=ws), got)
+    pr.check(pr.call(causal=causal, max_kv=50), causal)      # a wrong bound: nothing is cut, nothing left out
+    pr.check(pr.call(causal=causal, out_dtype=torch.float32), causal)
+
+
+def test_many_rows_of_many_sequences():
+    """More sequences than lanes, more tiles than fill the chip, and one long history among them."""
+    rng = np.random.default_rng(2)
+    lens = [int(x) for x in rng.integers(0, 60, size=300)]
+    new = [int(min(x, y)) for x, y in zip(lens, rng.integers(0, 80, size=300))]
+    lens[77], new[77] = 1500, 140
+    for heads, kv_heads in ((2, 1), (3, 3)):
+        pr = Problem("bf16", lens, new, heads, kv_heads, 32, 32, 16, seed=heads)
+        pr.check(pr.call())
+
+
 def test_large_batches():
     """Batches beyond one and beyond 64 sequences per lane of the schedule's scan."""
     rng = np.random.default_rng(0)
