@@ -924,6 +924,11 @@ _CODES = {torch.bfloat16: HSTU_BF16, torch.float32: HSTU_F32}
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+def _stream_of(index: int) -> int:
+    """The current stream of device `index`."""
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 class _Elsewhere:
     """The device and the stream of a call as torch's current ones, so that what the call allocates belongs to that stream (see
     _allocates_on_its_stream)."""
@@ -992,14 +997,14 @@ def _rotary_call(where, backward, tensors, inv_freq, seq_offsets, positions, int
         raise ValueError("one output per tensor")
     rows, outs, packed = None, [], []
     for i, t in enumerate(tensors):
-        r, heads, dim, stride = _rows(t, "tensors[%d]" % i, index, dtype)
+        r, heads, dim, stride = _rows(t, "every tensor", index, dtype)
         if rows is None:
             rows = r
         if out is None:
             o, ostride = torch.empty_like(t, memory_format=torch.contiguous_format), heads * dim
         else:
             o = out[i]
-            ro, ho, do, ostride = _rows(o, "out[%d]" % i, index, dtype)
+            ro, ho, do, ostride = _rows(o, "every output", index, dtype)
             if (ro, ho, do) != (r, heads, dim):
                 raise ValueError("out[%d] must have its tensor's shape" % i)
         if r != rows:
@@ -1013,7 +1018,7 @@ def _rotary_call(where, backward, tensors, inv_freq, seq_offsets, positions, int
     else:
         batch, pos, off = seq_offsets.shape[0] - 1, None, _index(seq_offsets, "seq_offsets", index)
     rc = load_library().hstu_rotary(_rotary_desc(inv_freq, interleaved, scale, index), backward, code, batch, rows, n,
-                                    b"".join(packed), pos, off, _stream(None))
+                                    b"".join(packed), pos, off, _stream_of(index))
     if rc != 0:
         raise HstuError(rc, where)
     return outs
@@ -1124,7 +1129,7 @@ def hstu_cache_append(cache: HstuPagedCache, k: torch.Tensor, v: torch.Tensor, s
     elif q_out is not None:
         raise ValueError("q_out without q")
     rc = load_library().hstu_cache_append(cache._address, desc, rows, tensor, k.data_ptr(), kstride, v.data_ptr(), vstride,
-                                          ts, off, _stream(None))
+                                          ts, off, _stream_of(index))
     if rc != 0:
         raise HstuError(rc, "hstu_cache_append")
     return q_out
@@ -1182,7 +1187,7 @@ def _paged_call(where, q, cache, seq_offsets, timestamps, ts_weights, groups_log
             raise ValueError("workspace must be contiguous and on the device of the call")
         ws, size = workspace, workspace.numel() * workspace.element_size()
     rc = lib.hstu_paged_attn_fwd(p, cache._address, bias, q.data_ptr(), stride, off, out.data_ptr(),
-                                 ws if type(ws) is int else ws.data_ptr(), size, _stream(None))
+                                 ws if type(ws) is int else ws.data_ptr(), size, _stream_of(index))
     if rc != 0:
         raise HstuError(rc, where)
     return out

@@ -88,7 +88,7 @@ struct Division {
   int whole, workers, grid, min_share;
   size_t front, bytes;  // records of cut tiles; these and partial results
 };
-constexpr int MANY_MEAN = 24;       // pairs per sequence and key/value head from which on the matrix cores bound the pass
+constexpr int MANY_MEAN = 8;        // pairs per sequence and key/value head beyond which tiles of 128 pairs are the better ones
 constexpr int MANY_WORKERS = 512;   // two workgroups per CU
 constexpr int MANY_SHARE = 128;
 constexpr int FEW_WORKERS = 1024;   // a one-wave worker per SIMD: 768..1536 are within 3 %, 2048 and 512 3 to 5 % behind
@@ -101,14 +101,17 @@ constexpr int TEAM_TILES = 512;     // team of waves, which joins its results it
 bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division* d) {
   const int group = p->num_heads / c->num_kv_heads;
   const int64_t cap = view_of(c).cap, pairs = p->new_rows * group;
-  d->many = c->dtype == HSTU_BF16 && pairs > (int64_t)MANY_MEAN * c->batch;
-  const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS;
+  const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap;
   // tiles of one head, at most: every sequence with rows may leave one of its tiles with a single pair
-  const int64_t tiles = (pairs + (qt - 1) * (c->batch < p->new_rows ? c->batch : p->new_rows)) / qt;
+  auto tiles_of = [&](int64_t qt) { return (pairs + (qt - 1) * (c->batch < p->new_rows ? c->batch : p->new_rows)) / qt; };
+  const bool team = keys * (c->d_qk + c->d_v) * size_of(c->dtype) <= TEAM_BYTES &&
+                    tiles_of(FEW_PAIRS) * c->num_kv_heads <= TEAM_TILES;
+  d->many = c->dtype == HSTU_BF16 && !team && pairs > (int64_t)MANY_MEAN * c->batch;
+  const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS, tiles = tiles_of(qt);
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
-  const int64_t keys = p->max_kv > 0 && p->max_kv < cap ? p->max_kv : cap, all = tiles * c->num_kv_heads;
-  d->whole = d->many ? keys <= MANY_SHARE : (keys * (c->d_qk + c->d_v) * size_of(c->dtype) <= TEAM_BYTES && all <= TEAM_TILES ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
+  const int64_t all = tiles * c->num_kv_heads;
+  d->whole = d->many ? keys <= MANY_SHARE : (team ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
   if (d->many) {
     // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)
