@@ -286,11 +286,16 @@ struct FewF32 {
     if constexpr (BIAS)
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[r] = t.wtab[bias_bucket(abs_diff(t.tq, (int)b.ts[r]), t.nb, t.f)];
+    f32x4 s2 = {0.f, 0.f, 0.f, 0.f};  // (two chains of half the length: less latency, less rounding)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int ks = 0; ks < KS; ks += 2)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e) {
         s = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, b.k[ks][e]), q[ks][e], s, 0, 0, 0);
+        s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, b.k[ks + 1][e]), q[ks + 1][e], s2, 0, 0, 0);
+      }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] += s2[r];
   }
   __device__ __forceinline__ void values(const TileCtx& t, int key) {
     const int g = (threadIdx.x & 63) >> 4;
