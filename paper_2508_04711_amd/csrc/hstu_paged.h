@@ -302,8 +302,8 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
 // There the tiles of one head read the same keys several times over, and what bounds the pass is whether they find them in
 // their XCD's L2: workers that run side by side have to stream the same keys at the same time.  So all tiles of a head are
 // cut at the same keys, into C pieces each (C: its sequence's length over a common share), units are ordered sequence, head,
-// piece, tile, and every workgroup takes one unit.  The share is the smallest with which every unit runs at once:
-// more units would be a second round of the chip for a few, and more partial results, of 64 KB each at d_v = 128.
+// piece, tile, and every workgroup takes one unit.  More units than run at
+// once would be a second round of the chip for a few of them, and more partial results, of 64 KB each at d_v = 128: see find_share.
 struct ManyUnit {
   int b, m, n, row0, tiles;
   int h, t;
@@ -346,7 +346,7 @@ struct Units {
     m = n = row0 = 0;
     const int64_t b0 = (int64_t)lane * chunk;
     int64_t keys = 0;
-    int tiles = 0;
+    int tiles = 0, longest = 0;
 #pragma unroll 4
     for (int i = 0; i < chunk; ++i) {
       const bool in = b0 + i < a.batch;
@@ -354,10 +354,11 @@ struct Units {
       const int t = in ? (int)(((int64_t)m * a.group + QT - 1) / QT) : 0;
       tiles += t;
       keys += t * (int64_t)n;
+      longest = t > 0 && n > longest ? n : longest;
     }
     const int all_tiles = __builtin_amdgcn_readlane(wave_scan(tiles), 63) * a.kv_heads;
     const int64_t all = lane64(wave_scan64(keys), 63) * a.kv_heads;
-    share = find_share(a, tiles, all_tiles, all);
+    share = find_share(a, tiles, all_tiles, all, longest);
     lane_units = lane_cut_units = lane_cut_tiles = 0;
 #pragma unroll 4
     for (int i = 0; i < chunk; ++i) {
@@ -375,21 +376,38 @@ struct Units {
     total_cut = __builtin_amdgcn_readlane(cut_tiles, 63);
   }
 
-  // The smallest share whose units have a place each in the chip's `workers` at once; where the tiles alone fill three quarters of
-  // them, in two rounds; where they fill more than most of two rounds, what one worker does of all the keys (only the
-  // longest sequences are then cut).
-  __device__ __forceinline__ int find_share(const PagedArgs& a, int tiles, int all_tiles, int64_t all) const {
-    const int room = 4 * all_tiles <= 3 * a.workers ? a.workers : 2 * a.workers;
-    const bool fit = 8 * (int64_t)all_tiles <= 7 * (int64_t)room;
-    // units <= keys / share + tiles
-    int64_t hi = fit ? quotient(all, room - all_tiles) + 64 : quotient(all, a.workers) + 1, lo = quotient(all, room);
-    if (fit && chunk == 1)
+  // The smallest share that makes at most `room` units (more than there are tiles).
+  __device__ __forceinline__ int64_t least_share(const PagedArgs& a, int tiles, int all_tiles, int64_t all, int room) const {
+    int64_t hi = quotient(all, room - all_tiles) + 64, lo = quotient(all, room);  // (units <= keys / share + tiles)
+    if (chunk == 1)
       while (hi - lo > 64) {
         const uint32_t mid = (uint32_t)((lo + hi) / 2);
         const int u = __builtin_amdgcn_readlane(wave_scan(tiles * (int)(((uint32_t)n + mid - 1) / mid)), 63) * a.kv_heads;
         if (u <= room) hi = mid; else lo = mid;
       }
-    return uniform32((int)(hi > a.min_share ? (hi < 0x7fffffc0 ? hi : 0x7fffffc0) : a.min_share));
+    return hi;
+  }
+  // Tiles that leave a quarter of the workers idle are cut until every worker has a unit.  Where they fill nearly one round of workers or
+  // two, what the call takes is estimated in keys per worker: uncut, the rounds that its tiles make (or the longest of them);
+  // cut into units of one round or two, their share (of two rounds of unequal units the second ends unevenly: an eighth more) and what writing
+  // and joining the parts takes.  Beyond, only tiles that hold more than an even part of all keys are cut.
+  __device__ __forceinline__ int find_share(const PagedArgs& a, int tiles, int all_tiles, int64_t all, int longest) const {
+    constexpr int JOIN_KEYS = 320;  // (10 us: a worker streams 64 keys in 2 us)
+    const int w = a.workers;
+    int64_t s;
+    if (4 * (int64_t)all_tiles <= 3 * (int64_t)w) {
+      s = least_share(a, tiles, all_tiles, all, w);
+    } else if (4 * (int64_t)all_tiles <= 7 * (int64_t)w) {
+      const int r = 8 * (int64_t)all_tiles <= 7 * (int64_t)w ? 1 : 2;
+      s = least_share(a, tiles, all_tiles, all, r * w);
+      longest = wave_max(longest);
+      const int64_t rounds = quotient(all, all_tiles) * ((all_tiles + w - 1) / w);
+      if ((r == 1 ? s : 2 * s + s / 4) + JOIN_KEYS >= (rounds > longest ? rounds : longest)) s = longest;
+    } else {
+      s = quotient(all, w) + 1;
+    }
+    s = s > a.min_share ? s : a.min_share;
+    return uniform32((int)(s < 0x7fffffc0 ? s : 0x7fffffc0));
   }
 
   // (u < total)

@@ -2,14 +2,14 @@
 //
 // With r (new row, query head) pairs per key/value head a row of the cache is worth r flops a byte: from about 128 on the
 // matrix cores bound the pass and not the memory.  So a worker is a workgroup of four waves, 32 pairs each, which shares the tiles
-// of 64 keys it streams through LDS: the forward pass's step (hstu_fwd_step.h) over pages.  Tiles of
+// of 64 keys it streams through LDS, with the forward pass's layouts (hstu_mfma.h).  Tiles of
 // 128 pairs are cut along the keys (Units, hstu_paged.h), so a call of two tiles fills the chip as one of hundreds does.
 //   - A wave-wide copy fills rows of one group of 16, which lies inside one page: its buffer descriptor is the group's
 //     rows, in scalar registers, and what lies behind the part's end or in a page that does not exist arrives as zeros.
 //   - The tiles of keys that every pair sees go through the pipelined step without any mask; the last few, which the causal
 //     diagonal crosses, through a loop that finishes a block at a time.
 //   - Consecutive workers (the tiles of one head over one range of keys) run on one XCD and find each other's tiles in its L2.
-#include "hstu_fwd_step.h"
+#include "hstu_mfma.h"
 #include "hstu_paged.h"
 
 namespace hstu {
@@ -78,6 +78,72 @@ struct PagedInit {
     }
   }
 };
+
+// One step of the pipeline over blocks of 32 keys: the matrix instructions of S(i + 1) = K(i + 1) Q^T and of O^T += V(i - 1)^T P(i - 1)^T,
+// and between them the SiLU of block i.  A wave issues one instruction at a time and waits where one needs the last
+// one's result, so the five instructions of an element's SiLU are spread over as many slots: what stands in a slot belongs to different
+// elements.  (4 x 512..1024 new rows over 4096..16384, H = 8: 148 us with an element's five instructions in one slot, 144 so.)  The empty
+// asm statements keep the compiler from moving the vector instructions behind the matrix instructions (166 us).
+template <int DQK, int DV, bool PV, class Init>
+__device__ __forceinline__ void many_step(const Init& init, const char* kn, int bn, const char* vp, int bp,
+                                          const RowAddr<DQK>& ra, const ColAddr<DV>& ca, const bf16x8 (&qreg)[DQK / 16],
+                                          const f32x16& s_in, f32x16& s_out, const bf16x8 (&p_prev)[2], bf16x8 (&p_cur)[2],
+                                          f32x16 (&oacc)[DV / 32], float c1) {
+  constexpr int KS = DQK / 16, NPV = DV / 16, NSL = KS > NPV ? KS : NPV;
+  constexpr int SLOTS = 2 * NSL, E = (16 + SLOTS - 1) / SLOTS;  // elements that enter per slot
+  constexpr int AHEAD = 3;  // operand reads in flight ahead of their use
+  bf16x8 ka[KS], va[NPV];
+  float x[16];
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto scale = [&](int h) {
+#pragma unroll
+    for (int i = h * E; i < (h + 1) * E && i < 16; ++i) x[i] = s_in[i] * c1;
+  };
+  auto silu = [&](int h) {  // slot h: elements of slots h, h - 1, h - 2, h - 3 one instruction further each
+#pragma unroll
+    for (int i = h * E; i < (h + 1) * E && i < 16; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(x[i]);
+      asm volatile("" : "+v"(x[i]));
+    }
+    scale(h + 1);
+    if (h >= 1)
+#pragma unroll
+      for (int i = (h - 1) * E; i < h * E && i < 16; ++i) x[i] = 1.0f + x[i];
+    if (h >= 2)
+#pragma unroll
+      for (int i = (h - 2) * E; i < (h - 1) * E && i < 16; ++i) {
+        x[i] = __builtin_amdgcn_rcpf(x[i]);
+        asm volatile("" : "+v"(x[i]));
+      }
+    if (h >= 3)
+#pragma unroll
+      for (int i = (h - 3) * E; i < (h - 2) * E && i < 16; ++i) x[i] = s_in[i] * x[i];
+  };
+  init(s_out);
+#pragma unroll
+  for (int m = 0; m < AHEAD; ++m) {
+    if (m < KS) ka[m] = ra.read(kn, bn, m);
+    if (PV && m < NPV) va[m] = ca.read(vp, bp * 2 + (m & 1), m >> 1);
+  }
+  scale(0);
+  fence();
+#pragma unroll
+  for (int m = 0; m < NSL; ++m) {
+    if (m < KS) s_out = mfma(ka[m], qreg[m], s_out);
+    if (m + AHEAD < KS) ka[m + AHEAD] = ra.read(kn, bn, m + AHEAD);
+    silu(2 * m);
+    fence();
+    if (PV && m < NPV) oacc[m >> 1] = mfma(va[m], p_prev[m & 1], oacc[m >> 1]);
+    if (PV && m + AHEAD < NPV) va[m + AHEAD] = ca.read(vp, bp * 2 + ((m + AHEAD) & 1), (m + AHEAD) >> 1);
+    silu(2 * m + 1);
+    fence();
+  }
+#pragma unroll
+  for (int h = SLOTS; h < SLOTS + 3; ++h) silu(h);
+  p_cur[0] = pack8(x);
+  p_cur[1] = pack8(x + 8);
+  fence();
+}
 
 template <int DQK, int DV, bool BIAS>
 __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArgs a) {
@@ -181,18 +247,12 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
 #pragma unroll
         for (int e = 0; e < 8; ++e) pb[x][y][e] = (__bf16)0.f;
     }
-    // No block is masked here, but the compiler must not know: without the step's branch it moves the SiLU's vector instructions
-    // behind the matrix instructions that they are to run beside (burst 165 us, MFMA_BEFORE).
-    int never = 0;
-    asm volatile("" : "+s"(never));
-    const bool mask = never != 0;
-    const auto none = [&] { return VisBefore{never, hh}; };
     if (wave_on) {
       init_of(0, 0)(sacc[0]);
 #pragma unroll
       for (int ks = 0; ks < DQK / 16; ++ks) sacc[0] = mfma(ra.read(kbuf(0), 0, ks), qreg[ks], sacc[0]);
-      fwd_step<DQK, DV, false>(init_of(0, 1), kbuf(0), 1, vbuf(0), 0, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0], oacc,
-                               c1, mask, none);
+      many_step<DQK, DV, false>(init_of(0, 1), kbuf(0), 1, vbuf(0), 0, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0], oacc,
+                               c1);
     }
     tile_barrier();
     auto iter = [&](int j, auto buf_tag) __attribute__((always_inline)) {
@@ -200,11 +260,11 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
       if (j + 2 <= T0 && j + 2 < T) copy_k(j + 2, B0);
       if (j + 1 < T) copy_v(j + 1, B1);
       if (wave_on) {
-        fwd_step<DQK, DV, true>(init_of(B1, 0), kbuf(B1), 0, vbuf(B0), 0, ra, ca, qreg, sacc[1], sacc[0], pb[0], pb[1], oacc,
-                                c1, mask, none);
+        many_step<DQK, DV, true>(init_of(B1, 0), kbuf(B1), 0, vbuf(B0), 0, ra, ca, qreg, sacc[1], sacc[0], pb[0], pb[1], oacc,
+                                c1);
         if (j + 1 < T0)
-          fwd_step<DQK, DV, true>(init_of(B1, 1), kbuf(B1), 1, vbuf(B0), 1, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0],
-                                  oacc, c1, mask, none);
+          many_step<DQK, DV, true>(init_of(B1, 1), kbuf(B1), 1, vbuf(B0), 1, ra, ca, qreg, sacc[0], sacc[1], pb[1], pb[0],
+                                  oacc, c1);
       }
       tile_copy_wait<0>();
       tile_barrier();
