@@ -89,7 +89,9 @@ struct Division {
   size_t front, bytes;  // records of cut tiles; these and partial results
 };
 constexpr int MANY_MEAN = 8;        // pairs per sequence and key/value head beyond which tiles of 128 pairs are the better ones
-constexpr int MANY_WORKERS = 512;   // two workgroups per CU
+// Workgroups that run at once: two per CU by registers and LDS, three of the smaller heads (4 x 512..1024 new rows over 4096..16384,
+// H = 8, d = 64: 106 us with two, 100 with three, 104 with four; d = 32: 85, 80, 78; 32 x 16..64 rows over 512..4096, d = 64: 48, 43, 52).
+int many_workers(const hstu_paged_cache* c) { return c->d_qk + c->d_v <= 160 ? 768 : 512; }
 constexpr int MANY_SHARE = 128;
 constexpr int FEW_WORKERS = 1024;   // a one-wave worker per SIMD: 768..1536 are within 3 %, 2048 and 512 3 to 5 % behind
 constexpr int MIN_SHARE = 64;       // keys that are worth a worker
@@ -116,10 +118,10 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   if (d->many) {
     // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)
     if (all >= (1ll << 30)) return false;
-    d->workers = MANY_WORKERS;
-    d->grid = (int)((all + 2 * MANY_WORKERS + 7) / 8 * 8);
-    d->front = align_up((size_t)MANY_WORKERS * sizeof(CutTile), 256);
-    d->bytes = d->whole ? 0 : d->front + (size_t)(2 * MANY_WORKERS) * qt * c->d_v * sizeof(float);
+    d->workers = many_workers(c);
+    d->grid = (int)((all + 2 * d->workers + 7) / 8 * 8);
+    d->front = align_up((size_t)d->workers * sizeof(CutTile), 256);
+    d->bytes = d->whole ? 0 : d->front + (size_t)(2 * d->workers) * qt * c->d_v * sizeof(float);
     return true;
   }
   int64_t workers = all;
