@@ -389,7 +389,8 @@ typedef struct {
 /* Turns the rows of up to 4 tensors (e.g. q and k, which may have different numbers of heads) in one launch.
  * positions: int32 [rows], or NULL: a row's place in its sequence, from seq_offsets int32 [batch + 1] (rows outside every sequence
  * are left alone).  backward = 1 turns by the opposite angles: src are the gradients of the turned rows, dst receives those of
- * the rows before the turn (the map is linear, so nothing else is needed).  No workspace. */
+ * the rows before the turn (the map is linear, so nothing else is needed).  An output may be its own tensor; it must not overlap
+ * another one's input or output.  No workspace. */
 int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype, int32_t batch, int64_t rows,
                 int32_t num_tensors, const hstu_rotary_tensor* tensors, const int32_t* positions,
                 const int32_t* seq_offsets, void* hip_stream);
@@ -403,7 +404,7 @@ int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype,
  * seq_lens[b] counts the rows of sequence b INCLUDING the new rows of the call; the m_b = seq_offsets[b + 1] - seq_offsets[b]
  * new rows are its last ones, at positions seq_lens[b] - m_b .. seq_lens[b] - 1.
  * Nothing of the cache is read on the host.  Whatever table and lengths hold, nothing outside the pages is touched: lengths
- * count as at least 0 and at most pages_per_seq * page_size, rows in a page whose id is not in 0 .. num_pages - 1 are dropped by an append and
+ * count as at least 0 and at most pages_per_seq * page_size (and 2^31 - 2^16), rows in a page whose id is not in 0 .. num_pages - 1 are dropped by an append and
  * count as zeros in the attention.  Rows behind a sequence's length and pages that the table does not name may hold anything,
  * NaN included. */
 typedef struct {

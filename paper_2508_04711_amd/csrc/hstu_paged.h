@@ -5,6 +5,9 @@
 
 namespace hstu {
 
+// Rows of a sequence that count at most (loops add up to a few thousand to a key's number).
+constexpr int32_t MAX_KEYS = 0x7fff0000;
+
 // A paged cache on the device.  Page p holds, per key/value head, `ps` rows: [heads][ps][d].
 struct PagedView {
   const char* k;              // pages of K and V
@@ -379,6 +382,7 @@ struct Units {
   // The smallest share that makes at most `room` units (more than there are tiles).
   __device__ __forceinline__ int64_t least_share(const PagedArgs& a, int tiles, int all_tiles, int64_t all, int room) const {
     int64_t hi = quotient(all, room - all_tiles) + 64, lo = quotient(all, room);  // (units <= keys / share + tiles)
+    hi = hi < 0x7fffffff ? hi : 0x7fffffff;
     if (chunk == 1)
       while (hi - lo > 64) {
         const uint32_t mid = (uint32_t)((lo + hi) / 2);

@@ -62,7 +62,7 @@ int check_cache(const hstu_paged_cache* c) {
   return HSTU_OK;
 }
 int check_cache_pointers(const hstu_paged_cache* c) {
-  if (!c->page_table || !c->seq_lens) return HSTU_ERR_NULL_PTR;
+  if ((c->pages_per_seq > 0 && !c->page_table) || !c->seq_lens) return HSTU_ERR_NULL_PTR;
   if (c->num_pages > 0 && (!c->k_pages || !c->v_pages)) return HSTU_ERR_NULL_PTR;
   return aligned16(c->k_pages) && aligned16(c->v_pages) && aligned16(c->ts_pages) ? HSTU_OK : HSTU_ERR_MISALIGNED;
 }
@@ -78,7 +78,7 @@ PagedView view_of(const hstu_paged_cache* c) {
   v.num_pages = (uint32_t)c->num_pages;
   v.ps_log2 = 31 - __builtin_clz((unsigned)c->page_size);
   const int64_t cap = (int64_t)c->pages_per_seq * c->page_size;
-  v.cap = cap < 0x7fffffff ? (int32_t)cap : 0x7fffffff;
+  v.cap = cap < MAX_KEYS ? (int32_t)cap : MAX_KEYS;
   return v;
 }
 
@@ -167,6 +167,9 @@ int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype,
   if (!positions && !seq_offsets) return HSTU_ERR_NULL_PTR;
   for (int i = 0; i < num_tensors; ++i)
     if (const int rc = check_row_pointers(&tensors[i])) return rc;
+  for (int i = 0; i < num_tensors; ++i)  // a tensor may be turned in place, not into another one's place
+    for (int j = 0; j < num_tensors; ++j)
+      if (i != j && (tensors[i].dst == tensors[j].dst || tensors[i].dst == tensors[j].src)) return HSTU_ERR_BAD_SHAPE;
   a.count = num_tensors;
   a.freq = rotary->inv_freq;
   a.rotary = rotary->rotary_dim; a.interleaved = rotary->interleaved ? 1 : 0;

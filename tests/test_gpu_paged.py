@@ -343,6 +343,42 @@ def test_a_history_served_in_steps_is_the_jagged_attention(dtype, bias):
         done = [a + m for a, m in zip(done, step)]
 
 
+def test_empty_calls():
+    """No rows, no sequences, no pages, no entries: nothing is launched, or zeros come back."""
+    off1, off0 = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pages = torch.zeros((3, 2, 16, 32), device="cuda")
+    table, lens = torch.zeros((1, 3), dtype=torch.int32, device="cuda"), torch.tensor([20], dtype=torch.int32, device="cuda")
+    none = torch.empty((0, 2, 32), device="cuda")
+    freq = hstu.hstu_rotary_frequencies(32)
+    cache = hstu.HstuPagedCache(pages, pages.clone(), table, lens)
+    assert hstu.hstu_paged_attn_fwd(none, cache, off1, 20, 0.1).shape == (0, 2, 32)
+    assert hstu.hstu_cache_append(cache, none, none, off1, q=none, inv_freq=freq).shape == (0, 2, 32)
+    assert hstu.hstu_rotary_fwd([none], freq, seq_offsets=off1)[0].shape == (0, 2, 32)
+    empty = hstu.HstuPagedCache(pages, pages.clone(), table[:0], lens[:0])
+    assert hstu.hstu_paged_attn_fwd(none, empty, off0, 20, 0.1).shape == (0, 2, 32)
+    one, off = torch.ones((1, 2, 32), device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for c in (hstu.HstuPagedCache(pages[:0], pages[:0], table, lens), hstu.HstuPagedCache(pages, pages, table[:, :0], lens)):
+        assert (hstu.hstu_paged_attn_fwd(one, c, off, 20, 0.1) == 0).all()
+        out = hstu.hstu_cache_append(c, one, one, off, q=one, inv_freq=freq)
+        assert torch.equal(out, hstu.hstu_rotary_fwd([one], freq, positions=lens - 1)[0]) and (pages == 0).all()
+
+
+def test_lengths_and_tables_of_nonsense():
+    """Offsets, lengths and ids that make no sense touch nothing outside: the call ends, other sequences' rows are right."""
+    pr = Problem("bf16", [50, 60, 70], [1, 1, 1], 2, 2, 32, 32, 16, fill=0.0)
+    cache, q = pr.cache(), pr.q.cuda()
+    off = torch.from_numpy(pr.off).cuda()
+    want = hstu.hstu_paged_attn_fwd(q, cache, off, 70, 0.1)
+    cache.seq_lens[1] = -(1 << 31)
+    cache.page_table[2] = -(1 << 31)
+    got = hstu.hstu_paged_attn_fwd(q, cache, off, 70, 0.1)
+    assert torch.equal(got[0], want[0]) and (got[1:] == 0).all()
+    before = cache.k_pages.clone()
+    hstu.hstu_cache_append(cache, q, q, off)
+    changed = (cache.k_pages != before).any(dim=3).any(dim=1)     # [page, slot]: the first sequence's new row alone
+    assert changed.sum() <= 1 and torch.equal(cache.k_pages[pr.table[0, 49 // 16], :, 49 % 16], q[0])
+
+
 def test_two_streams_at_once():
     """Two calls at the same time, each with its own workspace."""
     prs = [Problem("bf16", [3000, 100], [1, 1], 4, 4, 128, 128, 64, seed=s, fill=0.0) for s in (1, 2)]

@@ -78,6 +78,9 @@ def test_rotary_refusals(lib):
     assert call(tensors=(_tensor(src=FAKE + 8),)) == -7
     assert call(tensors=(None, _tensor(dst=FAKE + 2))) == -7
     assert call(off=None) == -1
+    x, y = 0x100000, 0x200000                                # one tensor into the other's place
+    assert call(tensors=(_tensor(src=x, dst=y), _tensor(src=y, dst=x))) == -2
+    assert call(tensors=(_tensor(src=x, dst=y), _tensor(src=0x300000, dst=y))) == -2
     assert call(rows=0, off=None) == 0 and call(batch=0) == 0   # nothing to do
 
 
