@@ -42,6 +42,7 @@ struct PagedArgs {
   int32_t grid;               // workgroups: enough for all workers or units
   int32_t whole;              // 1: every worker takes one tile, uncut; 2: ... and is a team of waves
   int32_t min_share;          // keys a worker takes at least
+  int32_t stream;             // the cached rows are more than the memory-side cache would keep: loads that allocate nothing there
 };
 
 // The schedule.  For one key/value head of one sequence the (new row, query head) pairs that read it are numbered

@@ -32,17 +32,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* p, int r
   return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows * row_bytes, 0x00020000);
 }
 
-template <int W>
-__device__ __forceinline__ void load_words(uint32_t (&dst)[W], __amdgpu_buffer_rsrc_t r, int voff, int soff) {
+// AUX 2: nontemporal (see PagedArgs::stream).
+template <int W, int AUX>
+__device__ __forceinline__ void load_words(uint32_t (&dst)[W], __amdgpu_buffer_rsrc_t r, int voff) {
   if constexpr (W == 4) {
-    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0);
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, voff, 0, AUX);
 #pragma unroll
     for (int i = 0; i < 4; ++i) dst[i] = x[i];
   } else if constexpr (W == 2) {
-    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, 0);
+    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, voff, 0, AUX);
     dst[0] = x[0]; dst[1] = x[1];
   } else {
-    dst[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, soff, 0);
+    dst[0] = __builtin_amdgcn_raw_buffer_load_b32(r, voff, 0, AUX);
   }
 }
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ Rows16 rows16(const PagedView& c, const PageIds& ids,
 // Block of 32 keys: two S^T products (keys 0..15 and 16..31 as rows), whose accumulators hold for the lane's pair the keys
 // 4 g + r and 16 + 4 g + r; those eight are the contraction index 8 g .. 8 g + 7 of the second product, so lane (i, g) loads
 // these eight rows of V, at elements VE * i .. of each (VE = d_v / 16), and product e of VE makes the output's elements VE * row + e.
-template <int DQK, int DV, bool BIAS>
+template <int DQK, int DV, bool BIAS, int AUX>
 struct FewBf16 {
   static constexpr int BK = 32, PARTS = 2, KS = DQK / 32, VE = DV / 16, VW = VE / 2;
   static constexpr int ROW_K = DQK * 2, ROW_V = DV * 2;
@@ -122,8 +123,8 @@ struct FewBf16 {
     for (int x = 0; x < 2; ++x) {
       const __amdgpu_buffer_rsrc_t rk = rows_rsrc(r[x].k, r[x].n, ROW_K);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) load_words<4>(b.k[x][ks], rk, ko + ks * 64, 0);
-      if constexpr (BIAS) load_words<4>(b.ts[x], rows_rsrc((const char*)r[x].ts, r[x].n, 4), to, 0);
+      for (int ks = 0; ks < KS; ++ks) load_words<4, AUX>(b.k[x][ks], rk, ko + ks * 64);
+      if constexpr (BIAS) load_words<4, AUX>(b.ts[x], rows_rsrc((const char*)r[x].ts, r[x].n, 4), to);
     }
   }
   __device__ __forceinline__ void fetch_v(const Rows16 (&r)[PARTS]) {
@@ -131,7 +132,7 @@ struct FewBf16 {
     for (int x = 0; x < 2; ++x) {
       const __amdgpu_buffer_rsrc_t rv = rows_rsrc(r[x].v, r[x].n, ROW_V);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) load_words<VW>(b.v[4 * x + e], rv, vo + e * ROW_V, 0);
+      for (int e = 0; e < 4; ++e) load_words<VW, AUX>(b.v[4 * x + e], rv, vo + e * ROW_V);
     }
   }
   // V's operand of output elements VE * row + e, rows behind `lim` of the block's keys left out where CUT.
@@ -231,7 +232,7 @@ struct FewBf16 {
 // Block of 16 keys.  The contraction over d_qk takes element 16 s + 4 g + e of a row at step (s, e); the one over keys takes key
 // 4 g + r at step r, which is what accumulator register r holds; lane (i, g) loads V's rows 4 g + r at elements
 // 16 VE j + VE i .. (VE = min(4, d_v / 16)), and product (j, e) makes the output's elements 16 VE j + VE * row + e.
-template <int DQK, int DV, bool BIAS>
+template <int DQK, int DV, bool BIAS, int AUX>
 struct FewF32 {
   static constexpr int BK = 16, PARTS = 1, KS = DQK / 16, VE = DV >= 64 ? 4 : 2, NJ = DV / (16 * VE);
   static constexpr int ROW_K = DQK * 4, ROW_V = DV * 4;
@@ -270,15 +271,15 @@ struct FewF32 {
   __device__ __forceinline__ void fetch_k(const Rows16 (&r)[PARTS]) {
     const __amdgpu_buffer_rsrc_t rk = rows_rsrc(r[0].k, r[0].n, ROW_K);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) load_words<4>(b.k[s], rk, ko + s * 64, 0);
-    if constexpr (BIAS) load_words<4>(b.ts, rows_rsrc((const char*)r[0].ts, r[0].n, 4), to, 0);
+    for (int s = 0; s < KS; ++s) load_words<4, AUX>(b.k[s], rk, ko + s * 64);
+    if constexpr (BIAS) load_words<4, AUX>(b.ts, rows_rsrc((const char*)r[0].ts, r[0].n, 4), to);
   }
   __device__ __forceinline__ void fetch_v(const Rows16 (&r)[PARTS]) {
     const __amdgpu_buffer_rsrc_t rv = rows_rsrc(r[0].v, r[0].n, ROW_V);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) load_words<VE>(b.v[e][j], rv, vo + e * ROW_V + j * 16 * VE * 4, 0);
+      for (int j = 0; j < NJ; ++j) load_words<VE, AUX>(b.v[e][j], rv, vo + e * ROW_V + j * 16 * VE * 4);
   }
   f32x4 s;
   __device__ __forceinline__ void scores(const TileCtx& t) {
@@ -351,8 +352,8 @@ struct FewF32 {
   static constexpr int OUT = 4 * VE * NJ;
 };
 
-template <bool F32, int DQK, int DV, bool BIAS>
-using Few = typename std::conditional<F32, FewF32<DQK, DV, BIAS>, FewBf16<DQK, DV, BIAS>>::type;
+template <bool F32, int DQK, int DV, bool BIAS, int AUX>
+using Few = typename std::conditional<F32, FewF32<DQK, DV, BIAS, AUX>, FewBf16<DQK, DV, BIAS, AUX>>::type;
 
 // Element of the output row that the lane's value x of result() is.
 template <bool F32, int DV>
@@ -409,9 +410,9 @@ __device__ __forceinline__ void stream_keys(F& f, const PagedArgs& a, const Tile
 }
 
 // NW = 1: workers are waves.  NW > 1: a worker is a workgroup whose waves share a tile's keys and add up their results in LDS.
-template <bool F32, int DQK, int DV, bool BIAS, int NW>
+template <bool F32, int DQK, int DV, bool BIAS, int NW, int AUX>
 __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
-  typedef Few<F32, DQK, DV, BIAS> F;
+  typedef Few<F32, DQK, DV, BIAS, AUX> F;
   constexpr int ES = F32 ? 4 : 2;
   __shared__ float wtab[BIAS ? MAX_TS_BUCKETS : 1];
   __shared__ float4 sums[NW > 1 ? NW * FEW_PAIRS * DV / 4 : 1];
@@ -548,16 +549,17 @@ __global__ void __launch_bounds__(REDUCE_THREADS) paged_reduce_kernel(PagedArgs 
 }
 
 constexpr int TEAM = 8;
-template <bool F32, int DQK, int DV, int NW>
+template <bool F32, int DQK, int DV, int NW, int AUX>
 hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.grid), block(64 * NW);
-  if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true, NW>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false, NW>), grid, block, 0, stream, a);
+  if (a.ts_w) hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, true, NW, AUX>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((paged_few_kernel<F32, DQK, DV, false, NW, AUX>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 template <bool F32, int DQK, int DV>
 hipError_t launch_few(const PagedArgs& a, hipStream_t stream) {
-  return a.whole == 2 ? launch_few<F32, DQK, DV, TEAM>(a, stream) : launch_few<F32, DQK, DV, 1>(a, stream);
+  if (a.whole == 2) return launch_few<F32, DQK, DV, TEAM, 0>(a, stream);
+  return a.stream ? launch_few<F32, DQK, DV, 1, 2>(a, stream) : launch_few<F32, DQK, DV, 1, 0>(a, stream);
 }
 template <bool F32, int DQK>
 hipError_t launch_few_dv(const PagedArgs& a, int d_v, hipStream_t stream) {

@@ -28,8 +28,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const char* base, in
 }
 
 // Copies the wave's share of keys [key, key + 64) into an LDS tile (swizzled like tile_copy_async); rows from `end` on
-// and rows without a page become zeros.  base: K or V pages; ids holds the tile's entries.
-template <int D>
+// and rows without a page become zeros.  AUX 2: nontemporal (PagedArgs::stream).  base: K or V pages; ids holds the tile's entries.
+template <int D, int AUX>
 __device__ __forceinline__ void page_copy_async(char* tile, const char* base, int64_t page_bytes, const PagedView& c,
                                                 const PageIds& ids, int h, int key, int end, int wave, int lane) {
   constexpr int RB = D * 2, CPR = D / 8, RPL = 64 / CPR, LOADS = ST / RPL;
@@ -41,7 +41,7 @@ __device__ __forceinline__ void page_copy_async(char* tile, const char* base, in
 #pragma unroll
     for (int i = 0; i < LOADS / MANY_WAVES; ++i) {
       const int idx = i * MANY_WAVES + wave;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, ((idx * RPL) & ~15) * RB, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, ((idx * RPL) & ~15) * RB, 0, AUX);
     }
     return;
   }
@@ -49,7 +49,7 @@ __device__ __forceinline__ void page_copy_async(char* tile, const char* base, in
   for (int i = 0; i < LOADS / MANY_WAVES; ++i) {
     const int idx = i * MANY_WAVES + wave;
     const __amdgpu_buffer_rsrc_t rsrc = page_rsrc(base, page_bytes, RB, c, ids, h, key + ((idx * RPL) & ~15), end, 16);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, 0, 0, AUX);
   }
 }
 
@@ -145,7 +145,7 @@ __device__ __forceinline__ void many_step(const Init& init, const char* kn, int 
   fence();
 }
 
-template <int DQK, int DV, bool BIAS>
+template <int DQK, int DV, bool BIAS, int AUX>
 __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArgs a) {
   constexpr int KB = ST * DQK * 2, VB = ST * DV * 2;
   // two buffers each, apart from each other, copies one tile ahead (see hstu_fwd_bf16)
@@ -213,12 +213,12 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
     const int key = sg.k0 + t * ST, last = key + ST - 1 < sg.k1 ? key + ST - 1 : sg.k1 - 1;
     // (V's copies are up to a tile behind K's: a refill starts there)
     if (!ids.holds(last >> a.c.ps_log2)) ids.fill(a.c, sg.b, (key - ST > sg.k0 ? key - ST : sg.k0) >> a.c.ps_log2, entries);
-    page_copy_async<DQK>(kbuf(buf), a.c.k, a.c.k_page, a.c, ids, sg.h, key, sg.k1, wave, lane);
+    page_copy_async<DQK, AUX>(kbuf(buf), a.c.k, a.c.k_page, a.c, ids, sg.h, key, sg.k1, wave, lane);
     if constexpr (BIAS)
       if (wave == 0) stamp_copy_async(tbuf(buf), a.c, ids, key, sg.k1, lane);
   };
   auto copy_v = [&](int t, int buf) __attribute__((always_inline)) {
-    page_copy_async<DV>(vbuf(buf), a.c.v, a.c.v_page, a.c, ids, sg.h, sg.k0 + t * ST, sg.k1, wave, lane);
+    page_copy_async<DV, AUX>(vbuf(buf), a.c.v, a.c.v_page, a.c, ids, sg.h, sg.k0 + t * ST, sg.k1, wave, lane);
   };
   auto init_of = [&](int buf, int blk) __attribute__((always_inline)) {
     return PagedInit<BIAS>{tbuf(buf) + blk * 32, wtab, tq, a.nb, a.f, hh};
@@ -399,12 +399,16 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
   }
 }
 
-template <int DQK, int DV>
+template <int DQK, int DV, int AUX>
 hipError_t launch_many(const PagedArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.grid), block(MANY_WAVES * 64);
-  if (a.ts_w) hipLaunchKernelGGL((paged_many_kernel<DQK, DV, true>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((paged_many_kernel<DQK, DV, false>), grid, block, 0, stream, a);
+  if (a.ts_w) hipLaunchKernelGGL((paged_many_kernel<DQK, DV, true, AUX>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((paged_many_kernel<DQK, DV, false, AUX>), grid, block, 0, stream, a);
   return hipGetLastError();
+}
+template <int DQK, int DV>
+hipError_t launch_many(const PagedArgs& a, hipStream_t stream) {
+  return a.stream ? launch_many<DQK, DV, 2>(a, stream) : launch_many<DQK, DV, 0>(a, stream);
 }
 template <int DQK>
 hipError_t launch_many_dv(const PagedArgs& a, int d_v, hipStream_t stream) {

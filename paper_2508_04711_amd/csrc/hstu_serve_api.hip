@@ -85,7 +85,7 @@ PagedView view_of(const hstu_paged_cache* c) {
 // How the attention's work is divided (see hstu_paged.h).
 struct Division {
   bool many;
-  int whole, workers, grid, min_share;
+  int whole, workers, grid, min_share, stream;
   size_t front, bytes;  // records of cut tiles; these and partial results
 };
 constexpr int MANY_MEAN = 8;        // pairs per sequence and key/value head beyond which tiles of 128 pairs are the better ones
@@ -98,6 +98,13 @@ constexpr int MIN_SHARE = 64;       // keys that are worth a worker
 constexpr int WHOLE_KEYS = 512;     // up to that many keys a tile is one worker's, uncut
 constexpr int TEAM_BYTES = 1 << 19; // up to that many bytes of keys and values a tile, and that many tiles, the worker is a
 constexpr int TEAM_TILES = 512;     // team of waves, which joins its results itself
+
+// Bytes of keys and values from which on the loads are nontemporal: half of the 256 MB of the memory-side cache, which then has nothing
+// to keep for the next call.  One new row over 307 MB (64 histories) 61.5 -> 54.4 us, 393 MB 75.8 -> 66.5, 144 MB with the bias 39.5 -> 35.4,
+// fp32 36.1 -> 32.5; 95 MB 23.6 either way; teams, which come nowhere near the memory's rate, lose (69 MB 18.2 -> 22.4).  Only where one
+// tile of pairs reads a row: 12 new rows over 150 MB 41.0 -> 37.7; several tiles lose (bursts 145 -> 152).
+constexpr int64_t STREAM_BYTES = 128 << 20;
+constexpr int STREAM_MEAN = 100;    // pairs per sequence and key/value head up to which most sequences have one tile of 128
 
 // false: sizes out of range
 bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division* d) {
@@ -113,6 +120,9 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   // the line of all work, in its own units, has to fit 62 bits
   if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
   const int64_t all = tiles * c->num_kv_heads;
+  const int64_t rows = (int64_t)c->batch * keys < c->num_pages * c->page_size ? (int64_t)c->batch * keys : c->num_pages * c->page_size;
+  d->stream = rows * c->num_kv_heads * (c->d_qk + c->d_v) * size_of(c->dtype) > STREAM_BYTES &&
+              pairs <= (int64_t)STREAM_MEAN * c->batch;
   d->whole = d->many ? keys <= MANY_SHARE : (team ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
   if (d->many) {
@@ -268,6 +278,7 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
   a.out_f32 = params->out_dtype == HSTU_F32;
   a.alpha = params->alpha; a.inv_n = 1.f / (float)params->max_len;
   a.workers = d.workers; a.grid = d.grid; a.whole = d.whole; a.min_share = d.min_share;
+  a.stream = d.stream;
   a.records = d.many && !d.whole ? d.workers : 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   {

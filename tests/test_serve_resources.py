@@ -9,10 +9,10 @@ from paper_2508_04711_amd import build as lib_build
 
 # name, waves per workgroup, workgroups per CU that the division of the work counts on
 EXPECTED = [
-    (r"paged_few_kernelILb[01]ELi\d+ELi\d+ELb[01]ELi1E", 1, 4),         # a one-wave worker per SIMD
-    (r"paged_few_kernelILb[01]ELi\d+ELi\d+ELb[01]ELi8E", 8, 1),
-    (r"paged_many_kernelILi\d+ELi\d+ELb[01]E", 4, 2),
-    (r"paged_many_kernelILi(32ELi(32|64|128)|64ELi(32|64)|128ELi32)ELb[01]E", 4, 3),
+    (r"paged_few_kernelILb[01]ELi\d+ELi\d+ELb[01]ELi1ELi[02]E", 1, 4),         # a one-wave worker per SIMD
+    (r"paged_few_kernelILb[01]ELi\d+ELi\d+ELb[01]ELi8ELi0E", 8, 1),
+    (r"paged_many_kernelILi\d+ELi\d+ELb[01]ELi[02]E", 4, 2),
+    (r"paged_many_kernelILi(32ELi(32|64|128)|64ELi(32|64)|128ELi32)ELb[01]ELi[02]E", 4, 3),
     (r"paged_reduce_kernelILi(16|128)ELi(32|64|128)E", 4, 8),
     (r"rotary_kernelILb[01]ELb[01]ELb[01]E", 4, 6),
 ]
