@@ -546,6 +546,7 @@ struct RotaryArgs {
   const int32_t* pos;    // positions of the rows, or null: places in their sequences
   const int32_t* off;
   int32_t batch, rows;
+  int32_t stream;        // nontemporal stores
   PagedView c;           // appending
   const int32_t* ts;     // timestamps of the rows, or null
 };

@@ -4,11 +4,15 @@
 // position * freq[j]:  y_a = x_a c - x_b s,  y_b = x_b c + x_a s,  c, s = scale * (cos, sin).  The map is linear and, up to
 // the scale, orthogonal: its gradient is the same turn by the opposite angle.
 //
-// Bound by reading and writing the rows once.  A thread takes eight pairs' worth of a row (two 16-byte chunks that hold whole
-// pairs in either layout; fp32: four pairs) and works their angles out once for up to four heads of a tensor, whose eight loads are in flight
+// Bound by reading and writing the rows once.  A thread takes eight pairs' worth of a row (two 16-byte chunks half the turned part
+// apart, which hold whole pairs in either layout; fp32: four pairs) and works their angles out once for up to four heads of a tensor, whose eight loads are in flight
 // together.  Angles: position * frequency / 2 pi in double precision, less the nearest whole turn, is exact to 1e-10 of a turn at
 // a million radians (1e-7 at the largest int32 position), where 32 bits lose a tenth of a turn (whole turns); the sine and cosine of what remains, at most an eighth of a turn after
 // taking off quarter turns, are their Taylor polynomials in fp32 (error below 2^-27).
+//
+// The rows are read with nontemporal loads (they are not needed again: q and k of 37117 rows, H = 4, and their gradients 64.7 -> 62.5 us),
+// and where a call writes more than the 256 MB of the memory-side cache, written so too (96016 rows, H = 8: 292 -> 278 us; appends, whose pages the
+// attention reads next, lose: 48.8 -> 63.6).
 #include "hstu_mfma.h"
 #include "hstu_paged.h"
 
@@ -104,7 +108,7 @@ struct Chunk {  // 16 bytes of a row
 
 // Rows of one tensor (blockIdx.y: the tensor and four of its heads).  A row of a head is d / (2 N) threads wide, each of which
 // takes the chunks c0 and c1 of it.
-template <bool F32, bool INTER, bool APPEND>
+template <bool F32, bool INTER, bool APPEND, bool STREAM>
 __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
   typedef Chunk<F32> C;
   constexpr int N = C::N;
@@ -158,25 +162,26 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
   const char* src = t.src + (int64_t)row * t.src_stride + (int64_t)head0 * t.d * (F32 ? 4 : 2);
   const int64_t src_head = (int64_t)t.d * (F32 ? 4 : 2);
 
-  const bool turned = t.rotate && c < a.rotary / (2 * N);
+  // The row's chunks: of the turned part, and of the rest (or of a row that is not turned), a thread takes one of the first half and the
+  // one at its place in the second half.
+  const int pairs = t.rotate ? a.rotary / (2 * N) : 0;  // threads that turn
+  const bool turned = c < pairs;
   if (!turned && t.src == t.dst) return;  // in place: what is not turned stays
-  // a thread's chunks: whole pairs, chunk c and the one half the rotated part behind it, or two neighbours
-  int c0 = 2 * c, c1 = 2 * c + 1;
-  if (!INTER && turned) {
-    c0 = c;
-    c1 = c + a.rotary / (2 * N);
-  }
+  const int c0 = turned ? c : pairs + c, c1 = turned ? c + pairs : wide + c;
   C p[ROT_HEADS], q[ROT_HEADS];
 #pragma unroll
   for (int h = 0; h < ROT_HEADS; ++h)
     if (h < heads) {
-      p[h].w = *(const u32x4*)(src + h * src_head + c0 * 16);
-      q[h].w = *(const u32x4*)(src + h * src_head + c1 * 16);
+      p[h].w = __builtin_nontemporal_load((const u32x4*)(src + h * src_head + c0 * 16));
+      q[h].w = __builtin_nontemporal_load((const u32x4*)(src + h * src_head + c1 * 16));
     }
   if (turned) {
     float cs[N], sn[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) turn_of((double)pos * a.freq[c * N + e], a.scale, a.sign, cs[e], sn[e]);
+    for (int e = 0; e < N; ++e) {
+      const int j = !INTER ? c * N + e : (e < N / 2 ? c0 * (N / 2) + e : c1 * (N / 2) + e - N / 2);  // (interleaved: a chunk's pairs are its own)
+      turn_of((double)pos * a.freq[j], a.scale, a.sign, cs[e], sn[e]);
+    }
 #pragma unroll
     for (int h = 0; h < ROT_HEADS; ++h)
       if (h < heads) {
@@ -205,8 +210,15 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
 #pragma unroll
   for (int h = 0; h < ROT_HEADS; ++h)
     if (h < heads) {
-      *(u32x4*)(dst + h * dst_head + c0 * 16) = p[h].w;
-      *(u32x4*)(dst + h * dst_head + c1 * 16) = q[h].w;
+      u32x4* d0 = (u32x4*)(dst + h * dst_head + c0 * 16);
+      u32x4* d1 = (u32x4*)(dst + h * dst_head + c1 * 16);
+      if constexpr (STREAM) {
+        __builtin_nontemporal_store(p[h].w, d0);
+        __builtin_nontemporal_store(q[h].w, d1);
+      } else {
+        *d0 = p[h].w;
+        *d1 = q[h].w;
+      }
     }
 }
 
@@ -220,13 +232,17 @@ hipError_t launch_rows(const RotaryArgs& a, int f32, hipStream_t stream) {
   }
   const int64_t per = ROT_THREADS / wide;
   const dim3 grid((unsigned)((a.rows + per - 1) / per), (unsigned)units), block(ROT_THREADS);
+#define HSTU_ROWS(F32, INTER)                                                                                       \
+  do {                                                                                                             \
+    if (!APPEND && a.stream) hipLaunchKernelGGL((rotary_kernel<F32, INTER, APPEND, !APPEND>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((rotary_kernel<F32, INTER, APPEND, false>), grid, block, 0, stream, a);                 \
+  } while (0)
   if (f32) {
-    if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<true, true, APPEND>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rotary_kernel<true, false, APPEND>), grid, block, 0, stream, a);
+    if (a.interleaved) HSTU_ROWS(true, true); else HSTU_ROWS(true, false);
   } else {
-    if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<false, true, APPEND>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rotary_kernel<false, false, APPEND>), grid, block, 0, stream, a);
+    if (a.interleaved) HSTU_ROWS(false, true); else HSTU_ROWS(false, false);
   }
+#undef HSTU_ROWS
   return hipGetLastError();
 }
 

@@ -186,6 +186,9 @@ int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype,
   a.scale = rotary->scale; a.sign = backward ? -1.f : 1.f;
   a.pos = positions; a.off = seq_offsets;
   a.batch = batch; a.rows = (int32_t)rows;
+  int64_t written = 0;
+  for (int i = 0; i < num_tensors; ++i) written += rows * tensors[i].num_heads * tensors[i].head_dim * size_of(dtype);
+  a.stream = written > (256ll << 20);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   TimedLaunch timed(14, stream);
   return launch_rotary(a, dtype == HSTU_F32, stream) == hipSuccess ? HSTU_OK : HSTU_ERR_HIP;
