@@ -32,14 +32,15 @@ struct PagedArgs {
   const float* ts_w;
   int32_t nb, f;
   void* o;                    // [rows][heads][d_v]
-  CutTile* cut;               // one per worker
-  float* partial;             // two slots per worker
+  const void* plan;           // large batches: the lanes' sums of Line or Units (paged_plan_kernel), or null
+  CutTile* cut;               // records of cut tiles, one per worker
+  float* partial;             // partial results, two per worker
   int32_t batch, rows, heads, kv_heads, group;
   int32_t causal, out_f32;
   float alpha, inv_n;
-  int32_t workers;            // a multiple of 8; many rows: the units that the work is cut into, about
+  int32_t workers;            // a multiple of 8; many rows: the workgroups that run at once
   int32_t records;            // many rows: records of cut tiles that there is room for
-  int32_t grid;               // workgroups: enough for all workers or units
+  int32_t grid;               // workgroups: enough for all workers; many rows: for all tiles and twice the workers
   int32_t whole;              // 1: every worker takes one tile, uncut; 2: ... and is a team of waves
   int32_t min_share;          // keys a worker takes at least
   int32_t stream;             // the cached rows are more than the memory-side cache would keep: loads that allocate nothing there
@@ -145,20 +146,26 @@ struct Line {
   __device__ __forceinline__ void init(const PagedArgs& a) {
     const int lane = threadIdx.x & 63;
     chunk = (a.batch + 63) >> 6;
-    sum = 0;
     m = n = row0 = 0;
-    const int64_t b0 = (int64_t)lane * chunk;
-    // (no branch on the sequence: the loads of several are in flight together)
-#pragma unroll 4
-    for (int i = 0; i < chunk; ++i) {
-      const bool in = b0 + i < a.batch;
-      const SeqWork s = read_work<QT>(a, in ? (int)b0 + i : a.batch - 1);
-      sum += in ? s.cost : 0;
-      m = s.m; n = s.n; row0 = s.row0;
-    }
-    sum *= a.kv_heads;
+    sum = a.plan ? ((const int64_t*)a.plan)[lane] : lane_sum(a, lane, 0, 1);
     incl = wave_scan64(sum);
     total = lane64(incl, 63);
+  }
+
+  // The cost of every `step`-th sequence of lane l's from i0 on.  Of a large batch a kernel of one workgroup sums it up, once for
+  // all workers; of a smaller one every worker does, which saves a launch.
+  __device__ __forceinline__ int64_t lane_sum(const PagedArgs& a, int l, int i0, int step) {
+    const int64_t b0 = (int64_t)l * chunk;
+    int64_t x = 0;
+    // (no branch on the sequence: the loads of several are in flight together)
+#pragma unroll 4
+    for (int i = i0; i < chunk; i += step) {
+      const bool in = b0 + i < a.batch;
+      const SeqWork s = read_work<QT>(a, in ? (int)b0 + i : a.batch - 1);
+      x += in ? s.cost : 0;
+      m = s.m; n = s.n; row0 = s.row0;
+    }
+    return x * a.kv_heads;
   }
 
   // The work of sequence b (uniform): from the lane that has read it already where every lane has one.
@@ -303,11 +310,11 @@ __device__ __forceinline__ Segment make_segment(const PagedArgs& a, const SeqWor
 }
 
 // ---- the schedule of calls of many rows ----------------------------------------------------------------------------------
-// There the tiles of one head read the same keys several times over, and what bounds the pass is whether they find them in
-// their XCD's L2: workers that run side by side have to stream the same keys at the same time.  So all tiles of a head are
-// cut at the same keys, into C pieces each (C: its sequence's length over a common share), units are ordered sequence, head,
-// piece, tile, and every workgroup takes one unit.  More units than run at
-// once would be a second round of the chip for a few of them, and more partial results, of 64 KB each at d_v = 128: see find_share.
+// There the tiles of one head read the same keys several times over: workers that run side by side stream the same keys at the same
+// time, and all but the first find them in their XCD's L2.  So all tiles of a head are cut at the same keys, into C pieces each
+// (C: its sequence's length over a common share), units are ordered sequence, head, piece, tile, and every workgroup takes one
+// unit.  More units than run at once would be a second round of the chip for a few of them, and more partial results, of 64 KB
+// each at d_v = 128: see find_share.
 struct ManyUnit {
   int b, m, n, row0, tiles;
   int h, t;
@@ -348,11 +355,33 @@ struct Units {
     const int lane = threadIdx.x & 63;
     chunk = (a.batch + 63) >> 6;
     m = n = row0 = 0;
-    const int64_t b0 = (int64_t)lane * chunk;
-    int64_t keys = 0;
-    int tiles = 0, longest = 0;
+    if (a.plan) {
+      const int4 sums = ((const int4*)a.plan)[lane];
+      lane_units = sums.x;
+      lane_cut_units = sums.y;
+      lane_cut_tiles = sums.z;
+      share = uniform32(sums.w);
+    } else {
+      int64_t tiles, keys;
+      int longest;
+      lane_tiles(a, lane, 0, 1, tiles, keys, longest);
+      lane_counts(a, lane, 0, 1, tiles, lane64(wave_scan64(tiles), 63), lane64(wave_scan64(keys), 63), longest);
+    }
+    units = wave_scan(lane_units);
+    cut_units = wave_scan(lane_cut_units);
+    cut_tiles = wave_scan(lane_cut_tiles);
+    total = __builtin_amdgcn_readlane(units, 63);
+    total_cut = __builtin_amdgcn_readlane(cut_tiles, 63);
+  }
+
+  // Every `step`-th sequence of lane l's from i0 on (large batches: see Line): its tiles of one head, their keys, and the most keys of one;
+  // and with the share its units.
+  __device__ __forceinline__ void lane_tiles(const PagedArgs& a, int l, int i0, int step, int64_t& tiles, int64_t& keys, int& longest) {
+    const int64_t b0 = (int64_t)l * chunk;
+    tiles = keys = 0;
+    longest = 0;
 #pragma unroll 4
-    for (int i = 0; i < chunk; ++i) {
+    for (int i = i0; i < chunk; i += step) {
       const bool in = b0 + i < a.batch;
       read(a, in ? (int)b0 + i : a.batch - 1, m, n, row0);
       const int t = in ? (int)(((int64_t)m * a.group + QT - 1) / QT) : 0;
@@ -360,12 +389,17 @@ struct Units {
       keys += t * (int64_t)n;
       longest = t > 0 && n > longest ? n : longest;
     }
-    const int all_tiles = __builtin_amdgcn_readlane(wave_scan(tiles), 63) * a.kv_heads;
-    const int64_t all = lane64(wave_scan64(keys), 63) * a.kv_heads;
-    share = find_share(a, tiles, all_tiles, all, longest);
+  }
+  __device__ __forceinline__ void lane_counts(const PagedArgs& a, int l, int i0, int step, int64_t tiles, int64_t all_tiles,
+                                              int64_t all_keys, int longest) {
+    const int64_t b0 = (int64_t)l * chunk;
     lane_units = lane_cut_units = lane_cut_tiles = 0;
+    share = 0x7fffffc0;
+    // (more tiles than the rows can make: the offsets do not ascend, and nothing is computed)
+    if (all_tiles > (a.grid - 2 * a.workers) / a.kv_heads) return;
+    share = find_share(a, (int)tiles, (int)all_tiles * a.kv_heads, all_keys * a.kv_heads, longest);
 #pragma unroll 4
-    for (int i = 0; i < chunk; ++i) {
+    for (int i = i0; i < chunk; i += step) {
       const bool in = b0 + i < a.batch;
       if (chunk > 1) read(a, in ? (int)b0 + i : a.batch - 1, m, n, row0);
       const Counts c = counts(a, in ? m : 0, n);
@@ -373,11 +407,6 @@ struct Units {
       lane_cut_units += c.cut_units;
       lane_cut_tiles += c.cut_tiles;
     }
-    units = wave_scan(lane_units);
-    cut_units = wave_scan(lane_cut_units);
-    cut_tiles = wave_scan(lane_cut_tiles);
-    total = __builtin_amdgcn_readlane(units, 63);
-    total_cut = __builtin_amdgcn_readlane(cut_tiles, 63);
   }
 
   // The smallest share that makes at most `room` units (more than there are tiles).
@@ -525,6 +554,9 @@ struct PageIds {
 // pairs of (q row, head) per tile and one-wave workers
 constexpr int FEW_PAIRS = 16;
 constexpr int MANY_PAIRS = 128;
+// The lanes' sums of Line or Units (PagedArgs::plan).
+constexpr int PLAN_BYTES = 64 * 16;
+hipError_t launch_paged_plan(const PagedArgs& a, int many, hipStream_t stream);
 hipError_t launch_paged_few(const PagedArgs& a, int dtype_f32, int d_qk, int d_v, hipStream_t stream);
 hipError_t launch_paged_many(const PagedArgs& a, int d_qk, int d_v, hipStream_t stream);
 // Adds up the partial results of cut tiles.  many: of the kernel with tiles of MANY_PAIRS.

@@ -505,6 +505,52 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
   if (!a.whole && lane == 0) a.cut[w] = cut;
 }
 
+// ---- large batches: the lanes' sums -----------------------------------------------------------------------------------------
+// One workgroup, PLAN_SUB threads per lane of the workers.  Bound by the round trips of its reads, 2 to 3 us at 1024 sequences;
+// without it every worker reads the whole batch.
+constexpr int PLAN_SUB = 16, PLAN_THREADS = 64 * PLAN_SUB;
+__device__ __forceinline__ int64_t sub_sum(int64_t x) {
+#pragma unroll
+  for (int i = 1; i < PLAN_SUB; i *= 2) x += __shfl_xor(x, i);
+  return x;
+}
+template <bool MANY>
+__global__ void __launch_bounds__(PLAN_THREADS) paged_plan_kernel(PagedArgs a, void* plan) {
+  const int l = threadIdx.x / PLAN_SUB, sub = threadIdx.x % PLAN_SUB;
+  if constexpr (!MANY) {
+    Line<FEW_PAIRS> line;
+    line.chunk = (a.batch + 63) >> 6;
+    const int64_t sum = sub_sum(line.lane_sum(a, l, sub, PLAN_SUB));
+    if (sub == 0) ((int64_t*)plan)[l] = sum;
+  } else {
+    __shared__ int64_t tiles[PLAN_THREADS / 64], keys[PLAN_THREADS / 64];
+    __shared__ int longest[PLAN_THREADS / 64];
+    Units<MANY_PAIRS> units;
+    units.chunk = (a.batch + 63) >> 6;  // (> 1: what a lane keeps of its one sequence is not read)
+    int64_t t, k;
+    int most;
+    units.lane_tiles(a, l, sub, PLAN_SUB, t, k, most);
+    t = lane64(wave_scan64(t), 63);
+    k = lane64(wave_scan64(k), 63);
+    most = wave_max(most);
+    const int wave = threadIdx.x >> 6;
+    keys[wave] = k;  // (the same in all lanes)
+    tiles[wave] = t;
+    longest[wave] = most;
+    __syncthreads();
+    t = k = 0;
+    most = 0;
+    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
+      k += keys[w];
+      t += tiles[w];
+      most = longest[w] > most ? longest[w] : most;
+    }
+    units.lane_counts(a, l, sub, PLAN_SUB, 0, uniform64(t), uniform64(k), most);
+    const int u = (int)sub_sum(units.lane_units), cu = (int)sub_sum(units.lane_cut_units), ct = (int)sub_sum(units.lane_cut_tiles);
+    if (sub == 0) ((int4*)plan)[l] = make_int4(u, cu, ct, units.share);
+  }
+}
+
 // ---- sum of the parts ------------------------------------------------------------------------------------------------------
 // Workgroup w adds up the parts of the tile of record w, if there is one, in their order.  Threads: one per four elements of the tile, in
 // blockIdx.y blocks, and where that leaves some over, runs of parts.
@@ -581,6 +627,13 @@ hipError_t launch_reduce(const PagedArgs& a, int d_v, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_paged_plan(const PagedArgs& a, int many, hipStream_t stream) {
+  void* plan = const_cast<void*>(a.plan);
+  if (many) hipLaunchKernelGGL((paged_plan_kernel<true>), dim3(1), dim3(PLAN_THREADS), 0, stream, a, plan);
+  else hipLaunchKernelGGL((paged_plan_kernel<false>), dim3(1), dim3(PLAN_THREADS), 0, stream, a, plan);
+  return hipGetLastError();
+}
 
 hipError_t launch_paged_few(const PagedArgs& a, int dtype_f32, int d_qk, int d_v, hipStream_t stream) {
   return dtype_f32 ? launch_few_d<true>(a, d_qk, d_v, stream) : launch_few_d<false>(a, d_qk, d_v, stream);

@@ -86,7 +86,8 @@ PagedView view_of(const hstu_paged_cache* c) {
 struct Division {
   bool many;
   int whole, workers, grid, min_share, stream;
-  size_t front, bytes;  // records of cut tiles; these and partial results
+  bool plan;                   // sums over the sequences come from a kernel of their own
+  size_t sums, front, bytes;   // bytes of these; and records of cut tiles; and partial results
 };
 constexpr int MANY_MEAN = 8;        // pairs per sequence and key/value head beyond which tiles of 128 pairs are the better ones
 // Workgroups that run at once: two per CU by registers and LDS, three of the smaller heads (4 x 512..1024 new rows over 4096..16384,
@@ -98,6 +99,11 @@ constexpr int MIN_SHARE = 64;       // keys that are worth a worker
 constexpr int WHOLE_KEYS = 512;     // up to that many keys a tile is one worker's, uncut
 constexpr int TEAM_BYTES = 1 << 19; // up to that many bytes of keys and values a tile, and that many tiles, the worker is a
 constexpr int TEAM_TILES = 512;     // team of waves, which joins its results itself
+
+// Sequences up to which every worker sums the batch up by itself; beyond, a launch does that once.  In turn without and with it, H = 4,
+// d = 64: one new row over 1..256 of 256, 512, 1024, 4096 sequences 12.1 / 14.8, 20.1 / 22.0, 40.1 / 35.9, 253 / 100 us; 32..64 rows over
+// up to 1024 of 128 and 256 34.7 / 38.0, 60.0 / 54.0; 16..32 over up to 512 of 512 and 1024 75 / 51, 198 / 87; d = 32, 4096: 2434 / 198.
+constexpr int PLAN_FEW = 512, PLAN_MANY = 128;
 
 // Bytes of keys and values from which on the loads are nontemporal: half of the 256 MB of the memory-side cache, which then has nothing
 // to keep for the next call.  One new row over 307 MB (64 histories) 61.5 -> 54.4 us, 393 MB 75.8 -> 66.5, 144 MB with the bias 39.5 -> 35.4,
@@ -117,21 +123,24 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
                     tiles_of(FEW_PAIRS) * c->num_kv_heads <= TEAM_TILES;
   d->many = c->dtype == HSTU_BF16 && !team && pairs > (int64_t)MANY_MEAN * c->batch;
   const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS, tiles = tiles_of(qt);
-  // the line of all work, in its own units, has to fit 62 bits
-  if ((double)c->num_kv_heads * (double)tiles * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
+  // the line of all work, in its own units, has to fit 62 bits, also where every sequence says that all rows are its own
+  const double most = (double)c->batch * ((double)pairs / (double)qt + 1.0);
+  if ((double)c->num_kv_heads * most * ((double)(cap + 2 * TILE_KEYS) * group + (double)pairs + 256.0) > 4e18) return false;
   const int64_t all = tiles * c->num_kv_heads;
   const int64_t rows = (int64_t)c->batch * keys < c->num_pages * c->page_size ? (int64_t)c->batch * keys : c->num_pages * c->page_size;
   d->stream = rows * c->num_kv_heads * (c->d_qk + c->d_v) * size_of(c->dtype) > STREAM_BYTES &&
               pairs <= (int64_t)STREAM_MEAN * c->batch;
   d->whole = d->many ? keys <= MANY_SHARE : (team ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
+  d->plan = c->batch > (d->many ? PLAN_MANY : PLAN_FEW);
+  d->sums = d->plan ? PLAN_BYTES : 0;
   if (d->many) {
     // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)
     if (all >= (1ll << 30)) return false;
     d->workers = many_workers(c);
     d->grid = (int)((all + 2 * d->workers + 7) / 8 * 8);
-    d->front = align_up((size_t)d->workers * sizeof(CutTile), 256);
-    d->bytes = d->whole ? 0 : d->front + (size_t)(2 * d->workers) * qt * c->d_v * sizeof(float);
+    d->front = d->sums + (d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256));
+    d->bytes = d->whole ? d->front : d->front + (size_t)(2 * d->workers) * qt * c->d_v * sizeof(float);
     return true;
   }
   int64_t workers = all;
@@ -140,8 +149,8 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
     workers = most < FEW_WORKERS ? (int64_t)most : FEW_WORKERS;
   }
   d->workers = d->grid = (int)((workers + 7) / 8 * 8);
-  d->front = d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256);
-  d->bytes = d->whole ? 0 : d->front + (size_t)d->workers * 2 * (size_t)qt * c->d_v * sizeof(float);
+  d->front = d->sums + (d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256));
+  d->bytes = d->whole ? d->front : d->front + (size_t)d->workers * 2 * (size_t)qt * c->d_v * sizeof(float);
   return true;
 }
 
@@ -273,7 +282,8 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
     a.nb = bias->num_buckets; a.f = bias->groups_log2;
   }
   a.o = o;
-  a.cut = (CutTile*)workspace;
+  a.plan = d.plan ? workspace : nullptr;
+  a.cut = (CutTile*)((char*)workspace + d.sums);
   a.partial = (float*)((char*)workspace + d.front);
   a.batch = cache->batch; a.rows = (int32_t)params->new_rows;
   a.heads = params->num_heads; a.kv_heads = cache->num_kv_heads; a.group = params->num_heads / cache->num_kv_heads;
@@ -284,6 +294,10 @@ int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_c
   a.stream = d.stream;
   a.records = d.many && !d.whole ? d.workers : 0;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (d.plan) {
+    TimedLaunch timed(3, stream);
+    if (launch_paged_plan(a, d.many, stream) != hipSuccess) return HSTU_ERR_HIP;
+  }
   {
     TimedLaunch timed(16, stream);
     const hipError_t e = d.many ? launch_paged_many(a, cache->d_qk, cache->d_v, stream)

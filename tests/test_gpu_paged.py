@@ -451,3 +451,39 @@ def test_refusals():
     with pytest.raises(hstu.HstuError) as e:
         hstu.hstu_paged_attn_fwd(q, small, off, 30, 0.1)
     assert e.value.status == -3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch", [128, 129, 512, 513, 1500])
+@pytest.mark.parametrize("hi,new_hi", [(60, 1), (700, 2), (90, 20), (600, 24)])
+def test_batches_on_both_sides_of_the_summing_kernel(dtype, batch, hi, new_hi):
+    """Short and long histories, one new row and many; sequences without rows at both ends and between."""
+    rng = np.random.default_rng(batch + hi)
+    lens = rng.integers(0, 20, size=batch)
+    lens[rng.integers(0, batch, size=12)] = hi
+    lens[[0, 1, batch - 1]] = 0
+    new = np.minimum(rng.integers(0, new_hi, size=batch, endpoint=True), lens)
+    if new_hi > 8:  # so many that most sequences have a tile of many pairs
+        lens = np.maximum(lens, new_hi)
+        new = rng.integers(new_hi // 2, new_hi, size=batch, endpoint=True)
+        new[[0, 1, batch - 1]] = 0
+    pr = Problem(dtype, [int(n) for n in lens], [int(n) for n in new], 2, 1, 32, 32, 16, seed=batch)
+    cache = pr.cache()
+    got = pr.call(cache)
+    pr.check(got)
+    assert torch.equal(got, pr.call(cache))
+
+
+@pytest.mark.parametrize("batch,rows", [(40, 700), (300, 700), (600, 3), (90, 3)])
+def test_offsets_that_do_not_ascend(batch, rows):
+    """Every second sequence says that all rows are its own: the call ends, nothing is written outside o, and the next call is right."""
+    pr = Problem("bf16", [300] * batch, [1] * batch, 1, 1, 32, 32, 16, fill=0.0)
+    cache = pr.cache()
+    off = torch.zeros(batch + 1, dtype=torch.int32, device="cuda")
+    off[1::2] = rows
+    buf = torch.full((rows + 128, 1, 32), 7.0, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((rows, 1, 32), dtype=torch.bfloat16, device="cuda")
+    for causal in (True, False):
+        hstu.hstu_paged_attn_fwd(q, cache, off, 300, 0.1, causal, out=buf[64:64 + rows])
+    assert (buf[:64] == 7).all() and (buf[64 + rows:] == 7).all()
+    pr.check(pr.call(cache))

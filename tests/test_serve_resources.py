@@ -13,6 +13,7 @@ EXPECTED = [
     (r"paged_few_kernelILb[01]ELi\d+ELi\d+ELb[01]ELi8ELi0E", 8, 1),
     (r"paged_many_kernelILi\d+ELi\d+ELb[01]ELi[02]E", 4, 2),
     (r"paged_many_kernelILi(32ELi(32|64|128)|64ELi(32|64)|128ELi32)ELb[01]ELi[02]E", 4, 3),
+    (r"paged_plan_kernelILb[01]E", 16, 1),
     (r"paged_reduce_kernelILi(16|128)ELi(32|64|128)E", 4, 8),
     (r"rotary_kernelILb[01]ELb[01]ELb[01]ELb[01]E", 4, 6),
 ]
