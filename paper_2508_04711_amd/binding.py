@@ -1052,8 +1052,14 @@ class HstuPagedCache:
     halves of one buffer [num_pages, 2, ...] do), page_table int32 [batch, pages_per_seq], seq_lens int32
     [batch]: rows of each sequence in the cache, the new rows of a call included; ts_pages int32 [num_pages, page_size]: the rows'
     timestamps, for models with the timestamp bias.  The cache is the caller's: table and lengths are read when a call
-    runs, so a program changes them in place (and captured calls see the change).
+    runs, so a program changes them in place (and captured calls see the change).  Other tensors are another HstuPagedCache.
     """
+    _BUFFERS = frozenset(("k_pages", "v_pages", "page_table", "seq_lens", "ts_pages"))
+
+    def __setattr__(self, name, value):
+        if name in self._BUFFERS and value is not self.__dict__.get(name, value):  # (cache.seq_lens += 1 sets the same tensor)
+            raise AttributeError("%s is changed in place; other tensors are another HstuPagedCache" % name)
+        object.__setattr__(self, name, value)
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
                  ts_pages: Optional[torch.Tensor] = None):

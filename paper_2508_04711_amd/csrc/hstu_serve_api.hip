@@ -221,6 +221,7 @@ int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rot
   if (!aligned16(k) || !aligned16(v)) return HSTU_ERR_MISALIGNED;
   if ((rc = check_cache_pointers(cache)) != HSTU_OK) return rc;
   if (q && (rc = check_row_pointers(q)) != HSTU_OK) return rc;
+  if (q && (q->dst == k || q->dst == v)) return HSTU_ERR_BAD_SHAPE;  // (may be q itself, not what others still read)
   RotaryArgs a = {};
   RotaryTensor& tk = a.t[a.count++];
   tk.src = (const char*)k; tk.src_stride = k_stride * size;

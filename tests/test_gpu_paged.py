@@ -487,3 +487,16 @@ def test_offsets_that_do_not_ascend(batch, rows):
         hstu.hstu_paged_attn_fwd(q, cache, off, 300, 0.1, causal, out=buf[64:64 + rows])
     assert (buf[:64] == 7).all() and (buf[64 + rows:] == 7).all()
     pr.check(pr.call(cache))
+
+
+def test_buffers_are_changed_in_place():
+    pr = Problem("bf16", [30, 20], [2, 1], 2, 2, 64, 64, 16, fill=0.0)
+    cache = pr.cache()
+    want = pr.call(cache)
+    cache.seq_lens -= 1
+    assert not torch.equal(pr.call(cache), want)
+    cache.seq_lens += 1
+    assert torch.equal(pr.call(cache), want)
+    for name in ("k_pages", "v_pages", "page_table", "seq_lens", "ts_pages"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, cache.seq_lens.clone())

@@ -100,6 +100,8 @@ def test_append_refusals(lib):
     assert call(ts=FAKE) == -1                                   # timestamps that the cache has no room for
     assert call(c=_cache(ts_pages=FAKE)) == -1                   # ... and a cache whose timestamps are not given
     assert call(rows=0, k=None) == 0 and call(c=_cache(batch=0), k=None) == 0
+    for kw in (dict(k=0x200000), dict(v=0x200000)):              # q's output over rows that are still read
+        assert call(q=_tensor(src=0x100000, dst=0x200000, ss=128, ds=128), **kw) == -2
 
 
 def test_attention_refusals(lib):
