@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
 }
 
 // ---- large batches: the lanes' sums -----------------------------------------------------------------------------------------
-// One workgroup, PLAN_SUB threads per lane of the workers.  Bound by the round trips of its reads, 2 to 3 us at 1024 sequences;
+// One workgroup, PLAN_SUB threads per lane of the workers.  Bound by the round trips of its reads: calls of 128 to 512 sequences take 2 to 3 us more with it;
 // without it every worker reads the whole batch.
 constexpr int PLAN_SUB = 16, PLAN_THREADS = 64 * PLAN_SUB;
 __device__ __forceinline__ int64_t sub_sum(int64_t x) {
