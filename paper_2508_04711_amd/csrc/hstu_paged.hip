@@ -15,7 +15,9 @@
 //     matched to them by the choice of the rows a lane loads), and V's rows are loaded whole, 16 bytes per lane, and transposed
 //     inside the lane (one byte permutation per register): nothing goes through LDS.
 //   - P enters the second product as two bf16 terms, whose sum is exact to 2^-17 of it, for 8 more matrix instructions per block
-//     in a loop that waits for memory: the result is off by its own rounding alone.
+//     in a loop that waits for memory: the result is off by its own rounding alone.  Two terms of opposite signs make NaN of an infinite
+//     value, and an infinite P has no second term, so a tile whose sums end up infinite or NaN is streamed once more, in a form that
+//     takes such terms apart (FewBf16::careful_values): what is finite, which is nearly everything, pays a test per tile.
 //   - Rows behind the part's end and rows of pages that do not exist lie outside the buffer descriptors: they arrive as zeros
 //     without traffic, so what such memory holds (other users' rows, NaN) has no way in.
 #include "hstu_mfma.h"
@@ -168,6 +170,7 @@ struct FewBf16 {
       for (int r = 0; r < 4; ++r) p[4 * x + r] = s[r];
     }
   }
+  template <bool CAREFUL>
   __device__ __forceinline__ void values(const TileCtx& t, int key) {
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -178,37 +181,15 @@ struct FewBf16 {
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = key + (e >> 2) * 16 + 4 * g + (e & 3) < t.lim ? p[e] : 0.f;
     }
+    if constexpr (CAREFUL) {
+      careful_values(t, key, masked);
+      return;
+    }
     bf16x8 hi, lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       hi[e] = (__bf16)p[e];
       lo[e] = (__bf16)(p[e] - (float)hi[e]);
-    }
-    if (masked) {
-      // Rows of V that some pairs see and others do not: an infinity or NaN there times a zero of P would reach the pairs that
-      // do not see it, so such a block is multiplied once per row position, without the rows behind it.
-      uint32_t bad = 0;
-#pragma unroll
-      for (int r = 0; r < 8; ++r)
-#pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          const uint32_t w = b.v[r][i];
-          bad |= (uint32_t)((w & 0x7f80u) == 0x7f80u) | (uint32_t)((w & 0x7f800000u) == 0x7f800000u);
-        }
-      if (__ballot(bad != 0) != 0) {
-        for (int lim = t.lim0; lim <= t.vis; ++lim) {
-#pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            const bf16x8 v = v_operand<true>(e, lim - key, g);
-            f32x4 part = acc[e];
-            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, part, 0, 0, 0);
-            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, part, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[e][r] = t.lim == lim ? part[r] : acc[e][r];
-          }
-        }
-        return;
-      }
     }
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
@@ -216,6 +197,48 @@ struct FewBf16 {
       acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, acc[e], 0, 0, 0);
       acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo, acc[e], 0, 0, 0);
     }
+  }
+  // The same where values or probabilities are infinite or NaN.  An infinite P has no second term, one that only rounds to infinity keeps
+  // the largest finite bf16 as its first; an infinite or NaN value is multiplied by the first term alone.  In a masked block, which
+  // some pairs see more of than others, such a value times a zero of P would reach the pairs that do not see it: the block is
+  // multiplied once per row position, without the rows behind it.
+  __device__ __forceinline__ void careful_values(const TileCtx& t, int key, bool masked) {
+    const int g = (threadIdx.x & 63) >> 4;
+    bf16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool finite = __builtin_fabsf(p[e]) <= 0x1.fffffep127f;
+      const float most = 0x1.fep127f;  // the largest finite bf16
+      const float h = finite ? __builtin_fminf(__builtin_fmaxf(p[e], -most), most) : p[e];
+      hi[e] = (__bf16)h;
+      lo[e] = (__bf16)(finite ? p[e] - (float)hi[e] : 0.f);
+    }
+    for (int lim = masked ? t.lim0 : t.vis; lim <= t.vis; ++lim) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const bf16x8 v = v_operand<true>(e, masked ? lim - key : BK, g);
+        u32x4 f = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t low = (f[w] & 0x7f80u) == 0x7f80u ? 0u : f[w] & 0xffffu;
+          f[w] = low | ((f[w] & 0x7f800000u) == 0x7f800000u ? 0u : f[w] & 0xffff0000u);
+        }
+        f32x4 part = acc[e];
+        part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi, part, 0, 0, 0);
+        part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), lo, part, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[e][r] = !masked || t.lim == lim ? part[r] : acc[e][r];
+      }
+    }
+  }
+  // Has any of the wave's pairs an infinite or NaN sum?  (No such term can leave the sum finite again.)
+  __device__ __forceinline__ bool lost() const {
+    float z = 0.f;
+#pragma unroll
+    for (int e = 0; e < VE; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z = __builtin_fmaf(acc[e][r], 0.f, z);
+    return __ballot(z != 0.f) != 0;
   }
   // The lane's part of its pair's output row: elements 4 VE g .. + 4 VE - 1.
   __device__ __forceinline__ void result(float (&x)[4 * VE]) const {
@@ -298,6 +321,7 @@ struct FewF32 {
 #pragma unroll
     for (int r = 0; r < 4; ++r) s[r] += s2[r];
   }
+  template <bool CAREFUL>
   __device__ __forceinline__ void values(const TileCtx& t, int key) {
     const int g = (threadIdx.x & 63) >> 4;
     float p[4];
@@ -315,7 +339,9 @@ struct FewF32 {
 #pragma unroll
           for (int e = 0; e < VE; ++e) bad |= (uint32_t)((b.v[r][j][e] & 0x7f800000u) == 0x7f800000u);
       }
-      if (__ballot(bad != 0) != 0) {  // (as in bf16)
+      // Values that some pairs see and others do not: an infinity or NaN there times a zero of P would reach the pairs that do not see
+      // it, so such a block is multiplied once per row position, without the rows behind it.
+      if (__ballot(bad != 0) != 0) {
         for (int lim = t.lim0; lim <= t.vis; ++lim)
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
@@ -380,7 +406,7 @@ __device__ __forceinline__ void store4(const PagedArgs& a, int64_t elem, float x
 }
 
 // Streams the keys [k0, k1) of head h of sequence b past the wave's pairs.
-template <class F>
+template <bool CAREFUL, class F>
 __device__ __forceinline__ void stream_keys(F& f, const PagedArgs& a, const TileCtx& t, int b, int h, int k0, int k1) {
   if (k0 >= k1) return;
   constexpr int BK = F::BK;
@@ -403,7 +429,7 @@ __device__ __forceinline__ void stream_keys(F& f, const PagedArgs& a, const Tile
     where(key + BK);
     f.fetch_k(r);
     __builtin_amdgcn_sched_barrier(0);
-    f.values(t, key);
+    f.template values<CAREFUL>(t, key);
     __builtin_amdgcn_sched_barrier(0);
     f.fetch_v(r);
   }
@@ -454,12 +480,21 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
     t.lim0 = sg.lim0;
     t.vis = sg.vis;
     t.lim = a.causal ? clampi((int64_t)pl.s.n - pl.s.m + row + 1, 0, pl.s.n) : pl.s.n;
-    f.start(on ? a.q + qrow * a.q_stride + (int64_t)head * DQK * ES : nullptr);
+    const char* const q = on ? a.q + qrow * a.q_stride + (int64_t)head * DQK * ES : nullptr;
+    auto stream = [&](int k0, int k1) __attribute__((always_inline)) {
+      f.start(q);
+      stream_keys<false>(f, a, t, pl.b, pl.h, k0, k1);
+      if constexpr (!F32)
+        if (__builtin_expect(f.lost(), 0)) {
+          f.start(q);
+          stream_keys<true>(f, a, t, pl.b, pl.h, k0, k1);
+        }
+    };
 
     if constexpr (NW > 1) {
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
       const int per = ((sg.k1 + 32 * NW - 1) / (32 * NW)) * 32, k0 = wave * per;  // (whole tiles: from key 0 on)
-      stream_keys(f, a, t, pl.b, pl.h, k0, k0 + per < sg.k1 ? k0 + per : sg.k1);
+      stream(k0, k0 + per < sg.k1 ? k0 + per : sg.k1);
       float x[F::OUT];
       f.result(x);
       float* slot = (float*)sums + (wave * FEW_PAIRS + i) * DV;
@@ -482,7 +517,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_few_kernel(PagedArgs a) {
       return;  // (one tile)
     }
 
-    stream_keys(f, a, t, pl.b, pl.h, sg.k0, sg.k1);
+    stream(sg.k0, sg.k1);
     if (on) {
       float x[F::OUT];
       f.result(x);
