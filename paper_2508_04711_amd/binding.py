@@ -1182,10 +1182,10 @@ def _paged_call(where, q, cache, seq_offsets, timestamps, ts_weights, groups_log
     lib = load_library()
     p = _paged_params(heads, max_len, alpha, causal, _code(odt), max_kv, rows)
     if workspace is None:
-        key = (heads, rows, max_kv)
-        if cache._need[0] != key:
-            cache._need = (key, lib.hstu_paged_attn_workspace_bytes(p, cache._address))
-        need = cache._need[1]
+        key, known = (heads, rows, max_kv), cache._need
+        if known[0] != key:  # (`known`, read once: another thread's call may replace what the cache remembers at any time)
+            known = cache._need = (key, lib.hstu_paged_attn_workspace_bytes(p, cache._address))
+        need = known[1]
         # (256: the call cuts nothing and touches no workspace)
         ws, size = (out.data_ptr(), 0) if need <= 256 else (torch.empty(need, dtype=torch.uint8, device=q.device), need)
     else:
