@@ -1184,7 +1184,9 @@ def _paged_call(where, q, cache, seq_offsets, timestamps, ts_weights, groups_log
     if workspace is None:
         key, known = (heads, rows, max_kv), cache._need
         if known[0] != key:  # (`known`, read once: another thread's call may replace what the cache remembers at any time)
-            known = cache._need = (key, lib.hstu_paged_attn_workspace_bytes(p, cache._address))
+            known = (key, lib.hstu_paged_attn_workspace_bytes(p, cache._address))
+            if known[1]:  # (0: the library refuses this call, not every call of its shape)
+                cache._need = known
         need = known[1]
         # (256: the call cuts nothing and touches no workspace)
         ws, size = (out.data_ptr(), 0) if need <= 256 else (torch.empty(need, dtype=torch.uint8, device=q.device), need)

@@ -66,3 +66,17 @@ def test_a_call_between_query_and_launch_does_not_change_the_workspace(calls, mo
     _call(cache, 5)
     assert sorted(rows for rows, _, _ in calls) == [5, 5, 600, 600]
     assert all(size == need > 256 for _, size, need in calls), calls
+
+
+@pytest.mark.parametrize("bad", [dict(max_len=0), dict(alpha=float("inf")), dict(out_dtype=torch.bfloat16)])
+def test_a_refused_call_leaves_nothing_behind(calls, bad):
+    """The library's query gives 0 for a call that it refuses: the next call of the same shape asks again."""
+    dtype = torch.float32 if "out_dtype" in bad else torch.bfloat16
+    cache = binding.HstuPagedCache(*(_on_device(80, 4, 64, 128, dtype=dtype) for _ in range(2)),
+                                   _on_device(5, 80, dtype=torch.int32), _on_device(5, dtype=torch.int32))
+    off, q = _on_device(6, dtype=torch.int32), _on_device(7, 4, 128, dtype=dtype)
+    with pytest.raises(binding.HstuError) as e:
+        binding.hstu_paged_attn_fwd(q, cache, off, bad.get("max_len", 100), bad.get("alpha", 0.1), out_dtype=bad.get("out_dtype"))
+    assert e.value.status == -2
+    binding.hstu_paged_attn_fwd(q, cache, off, 100, 0.1)
+    assert calls[-1][0] == 7 and calls[-1][1] == calls[-1][2] > 256
