@@ -29,6 +29,7 @@ def calls(monkeypatch):
 
     class Library:
         hstu_paged_attn_workspace_bytes = staticmethod(lib.hstu_paged_attn_workspace_bytes)
+        hstu_attn_status_string = staticmethod(lib.hstu_attn_status_string)
 
         @staticmethod
         def hstu_paged_attn_fwd(params, cache, bias, q, q_stride, off, o, ws, size, stream):
