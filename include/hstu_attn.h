@@ -429,7 +429,9 @@ typedef struct {
 /* Writes the new rows of k [new_rows, num_kv_heads, d_qk] and v [new_rows, num_kv_heads, d_v] (rows k_stride / v_stride
  * elements apart) to their places in the cache, the keys turned by their positions where `rotary` is not NULL.  q, if not
  * NULL, is turned in the same launch (rows of head_dim d_qk; its output may be q itself and must not overlap k or v).  timestamps: int32 [new_rows], required iff the cache holds
- * timestamps.  A row without a place (negative position, no entry or no such page) is dropped.  The pages of the new rows of
+ * timestamps.  A row without a place (negative position, no entry or no such page) is dropped.  A length beyond the table's room counts as the
+ * room here as in the attention: the new rows go to the last places that there are, over what they held.  (A table without any entries
+ * has no places; there rows are turned by the positions that the length says.)  The pages of the new rows of
  * different sequences have to be different ones. */
 int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rotary, int64_t new_rows,
                       const hstu_rotary_tensor* q, const void* k, int64_t k_stride, const void* v, int64_t v_stride,

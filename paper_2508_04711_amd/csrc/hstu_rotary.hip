@@ -133,14 +133,15 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
   } else {
     b = find_sequences(a.off, a.batch, row0, a.rows, shift);
     // (rows outside every sequence are left alone)
-    const int s = a.off[b], e = a.off[b + 1];
+    int s, e;
+    seq_range(a.off, b, a.rows, s, e);
     on = in && row >= s && row < e;
     pos = row - s;
     if constexpr (APPEND) {
-      // (in 64 bits: wrong offsets or lengths must not wrap into a valid position)
-      const int64_t p = (int64_t)a.c.lens[b] - e + row;
-      on = on && p >= -0x80000000ll && p <= 0x7fffffffll;
-      pos = (int)p;
+      // Lengths and offsets count as the attention counts them, wrong ones too: a row's place is the one that the attention takes for its
+      // own.  (A sequence without entries has no places; its rows are turned by the positions that its length says.)
+      const int64_t n = clampi(a.c.lens[b], 0, a.c.cap > 0 ? a.c.cap : MAX_KEYS);
+      pos = (int)(n - e + row);
     }
   }
   // where the row goes
