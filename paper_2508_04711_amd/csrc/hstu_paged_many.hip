@@ -38,11 +38,14 @@ __device__ __forceinline__ void page_copy_async(char* tile, const char* base, in
   const int row = ((wave * RPL) & 15) + lane / CPR, voff = row * RB + (((lane % CPR) ^ swz<D>(row)) << 4);
   if (c.ps_log2 >= 6) {  // the tile is in one page (its first key is a multiple of 64): one descriptor for all of it
     const __amdgpu_buffer_rsrc_t rsrc = page_rsrc(base, page_bytes, RB, c, ids, h, key, end, ST);
+    // (The group's offset in the vector register: the descriptor's bound is not defined for the scalar offset, and a
+    // tile that ends inside the page, or has no page, has groups that lie behind it.)
+    int group = voff + ((wave * RPL) & ~15) * RB;
+    asm volatile("" : "+v"(group));  // (worked out at every copy: the loop has no registers for all groups' offsets)
 #pragma unroll
-    for (int i = 0; i < LOADS / MANY_WAVES; ++i) {
-      const int idx = i * MANY_WAVES + wave;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + idx * 1024), 16, voff, ((idx * RPL) & ~15) * RB, 0, AUX);
-    }
+    for (int i = 0; i < LOADS / MANY_WAVES; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, HSTU_LDS(void, tile + (i * MANY_WAVES + wave) * 1024), 16,
+                                               group + i * MANY_WAVES * RPL * RB, 0, 0, AUX);
     return;
   }
 #pragma unroll
