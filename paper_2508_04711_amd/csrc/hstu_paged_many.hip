@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
       const VisBefore vis(lim - 1 - key, hl);
 #pragma unroll
       for (int r = 0; r < 16; ++r) p[r] = vis(r) ? s[r] * sigmoid_scaled(s[r], c1) : 0.f;
-      const bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
+      bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
       // Rows of V that some pairs of the wave see and others do not: an infinity or NaN there times a zero of P would reach
       // the pairs that do not see it.  So the product takes the rows before the first such one alone ...
       int first = 32;  // (rows of the block; a lane's operand holds four runs of four of them)
@@ -350,6 +350,15 @@ __global__ void __launch_bounds__(MANY_WAVES * 64, 2) paged_many_kernel(PagedArg
         keep[2 * x] = c >= 2 ? ~0u : (c == 1 ? 0xffffu : 0u);
         keep[2 * x + 1] = c >= 4 ? ~0u : (c == 3 ? 0xffffu : 0u);
       }
+      // (both factors of the rows that are left out: theirs may be infinite too)
+      u32x4 w0 = __builtin_bit_cast(u32x4, p0), w1 = __builtin_bit_cast(u32x4, p1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w0[e] &= keep[e];
+        w1[e] &= keep[4 + e];
+      }
+      p0 = __builtin_bit_cast(bf16x8, w0);
+      p1 = __builtin_bit_cast(bf16x8, w1);
 #pragma unroll
       for (int c = 0; c < DV / 32; ++c)
 #pragma unroll

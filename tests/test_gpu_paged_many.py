@@ -1,12 +1,13 @@
 """The kernel of many new rows (tiles of 128 pairs, bf16) at every pair of head dimensions, with pages smaller than a tile of keys, as
-large and larger, causal or not, and with the timestamp bias.  Every call here is asserted to be that kernel's, with its tiles cut
-along the keys."""
+large and larger, causal or not, with the timestamp bias, and with infinities and NaN among the values.  Every call here is
+asserted to be that kernel's, with its tiles cut along the keys."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2508_04711_amd as hstu
 from test_gpu_paged import NAN, Problem
+from test_gpu_paged_special import INF, _check, _row
 
 pytestmark = pytest.mark.gpu
 
@@ -63,6 +64,26 @@ def test_pages_that_do_not_exist(ps, causal):
     pr.table[0, 1], pr.table[0, 1300 // ps] = -1, pr.pages
     pr.table[1, 299 // ps] = -(1 << 31)
     pr.check(_many(pr, pr.cache(), causal=causal), causal)
+
+
+@pytest.mark.parametrize("dqk,dv", [(32, 32), (128, 128), (64, 128), (128, 32)])
+@pytest.mark.parametrize("ps", [16, 64])
+@pytest.mark.parametrize("causal", [True, False])
+def test_infinities_and_nan(dqk, dv, ps, causal):
+    """In rows that all new rows see and, causal, in rows that only some of a tile's see: they reach those that see them, as what the
+    definition makes of them."""
+    pr = _problem(dqk, dv, ps, causal, seed=5)
+    n, m = pr.lens[0], pr.new[0]
+    for p, element, value in ((7, 0, INF), (700, 1, -INF), (n - 1, 2, INF), (n - 40, 3, -INF), (n - 41, 30, NAN), (n - 3, 4, NAN)):
+        _row(pr, pr.vp, 0, p)[:, element] = value
+    _row(pr, pr.vp, 1, 299)[0, 5] = -INF
+    pr.q[:m, :, 6] = pr.q[:m, :, 6].abs() + 0.125
+    _row(pr, pr.kp, 0, n - 2)[:, 6] = INF       # an infinite probability of the last two new rows
+    pr.q[m - 1, 0, 6] = -1.0
+    finite, o = _check(pr, _many(pr, pr.cache(), causal=causal), causal)
+    if causal:
+        assert finite[:m - 41, :, [2, 3, 4, 30]].all() and not finite[m - 40:m, :, 30].any()
+        assert np.isnan(o[m - 1, 0]).all() and (o == INF).any() and (o == -INF).any()
 
 
 @pytest.mark.parametrize("batch", [40, 300])
