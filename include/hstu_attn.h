@@ -390,7 +390,8 @@ typedef struct {
  * positions: int32 [rows], or NULL: a row's place in its sequence, from seq_offsets int32 [batch + 1] (rows outside every sequence
  * are left alone).  backward = 1 turns by the opposite angles: src are the gradients of the turned rows, dst receives those of
  * the rows before the turn (the map is linear, so nothing else is needed).  An output may be its own tensor; it must not overlap
- * another one's input or output.  No workspace. */
+ * another one's input or output.  rows: below 2^31, and rows * head_dim below 2^36 (bf16) or 2^35 (fp32), less 2^15, of every tensor.  No
+ * workspace. */
 int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype, int32_t batch, int64_t rows,
                 int32_t num_tensors, const hstu_rotary_tensor* tensors, const int32_t* positions,
                 const int32_t* seq_offsets, void* hip_stream);
@@ -432,7 +433,7 @@ typedef struct {
  * timestamps.  A row without a place (negative position, no entry or no such page) is dropped.  A length beyond the table's room counts as the
  * room here as in the attention: the new rows go to the last places that there are, over what they held.  (A table without any entries
  * has no places; there rows are turned by the positions that the length says.)  The pages of the new rows of
- * different sequences have to be different ones. */
+ * different sequences have to be different ones.  new_rows: limited as in hstu_rotary. */
 int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rotary, int64_t new_rows,
                       const hstu_rotary_tensor* q, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                       const int32_t* timestamps, const int32_t* seq_offsets, void* hip_stream);

@@ -38,6 +38,11 @@ int check_row_pointers(const hstu_rotary_tensor* t) {
   return aligned16(t->src) && aligned16(t->dst) ? HSTU_OK : HSTU_ERR_MISALIGNED;
 }
 
+// Threads that a launch may have in one direction of its grid.
+constexpr int64_t MAX_THREADS = (1ll << 32) - 1;
+// Do `rows` rows of head_dim elements fit a launch of the kernel that turns and appends rows (d / 16 threads a row, fp32 d / 8)?
+bool rows_fit(int64_t rows, int head_dim, int64_t size) { return (rows + 255) * (head_dim * size / 32) <= MAX_THREADS; }
+
 RotaryTensor tensor_of(const hstu_rotary_tensor* t, int64_t size) {
   RotaryTensor r = {};
   r.src = (const char*)t->src; r.dst = (char*)t->dst;
@@ -121,7 +126,9 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   auto tiles_of = [&](int64_t qt) { return (pairs + (qt - 1) * (c->batch < p->new_rows ? c->batch : p->new_rows)) / qt; };
   const bool team = keys * (c->d_qk + c->d_v) * size_of(c->dtype) <= TEAM_BYTES &&
                     tiles_of(FEW_PAIRS) * c->num_kv_heads <= TEAM_TILES;
-  d->many = c->dtype == HSTU_BF16 && !team && pairs > (int64_t)MANY_MEAN * c->batch;
+  // (workgroups of 256 threads; beyond what a launch may have, one-wave workers on cut lines)
+  d->many = c->dtype == HSTU_BF16 && !team && pairs > (int64_t)MANY_MEAN * c->batch &&
+            (tiles_of(MANY_PAIRS) * c->num_kv_heads + 2 * many_workers(c) + 8) * 256 <= MAX_THREADS;
   const int64_t qt = d->many ? MANY_PAIRS : FEW_PAIRS, tiles = tiles_of(qt);
   // the line of all work, in its own units, has to fit 62 bits, also where every sequence says that all rows are its own
   const double most = (double)c->batch * ((double)pairs / (double)qt + 1.0);
@@ -130,13 +137,12 @@ bool divide(const hstu_paged_attn_params* p, const hstu_paged_cache* c, Division
   const int64_t rows = (int64_t)c->batch * keys < c->num_pages * c->page_size ? (int64_t)c->batch * keys : c->num_pages * c->page_size;
   d->stream = rows * c->num_kv_heads * (c->d_qk + c->d_v) * size_of(c->dtype) > STREAM_BYTES &&
               pairs <= (int64_t)STREAM_MEAN * c->batch;
-  d->whole = d->many ? keys <= MANY_SHARE : (team ? 2 : (keys <= WHOLE_KEYS && all < (1ll << 30) ? 1 : 0));
+  d->whole = d->many ? keys <= MANY_SHARE : (team ? 2 : (keys <= WHOLE_KEYS && (all + 8) * 64 <= MAX_THREADS ? 1 : 0));
   d->min_share = d->many ? MANY_SHARE : MIN_SHARE;
   d->plan = c->batch > (d->many ? PLAN_MANY : PLAN_FEW);
   d->sums = d->plan ? PLAN_BYTES : 0;
   if (d->many) {
     // every uncut tile is a unit, and cut ones make at most twice as many as there are workers, two or more a tile (see Units)
-    if (all >= (1ll << 30)) return false;
     d->workers = many_workers(c);
     d->grid = (int)((all + 2 * d->workers + 7) / 8 * 8);
     d->front = d->sums + (d->whole ? 0 : align_up((size_t)d->workers * sizeof(CutTile), 256));
@@ -180,6 +186,7 @@ int hstu_rotary(const hstu_rotary_desc* rotary, int32_t backward, int32_t dtype,
     int rc = check_rows(&tensors[i], size_of(dtype));
     if (rc == HSTU_OK) rc = check_rotary(rotary, tensors[i].head_dim);
     if (rc != HSTU_OK) return rc;
+    if (!rows_fit(rows, tensors[i].head_dim, size_of(dtype))) return HSTU_ERR_BAD_SHAPE;
     a.t[i] = tensor_of(&tensors[i], size_of(dtype));
   }
   if (rows == 0 || (!positions && batch == 0)) return HSTU_OK;
@@ -208,8 +215,9 @@ int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rot
                       const int32_t* timestamps, const int32_t* seq_offsets, void* hip_stream) {
   int rc = check_cache(cache);
   if (rc != HSTU_OK) return rc;
-  if (new_rows < 0 || new_rows >= (1ll << 31)) return HSTU_ERR_BAD_SHAPE;
   const int64_t size = size_of(cache->dtype);
+  if (new_rows < 0 || new_rows >= (1ll << 31) || !rows_fit(new_rows, cache->d_qk > cache->d_v ? cache->d_qk : cache->d_v, size))
+    return HSTU_ERR_BAD_SHAPE;
   if (rotary && (rc = check_rotary(rotary, cache->d_qk)) != HSTU_OK) return rc;
   if (!stride_ok(k_stride, (int64_t)cache->num_kv_heads * cache->d_qk, size) ||
       !stride_ok(v_stride, (int64_t)cache->num_kv_heads * cache->d_v, size))
