@@ -225,7 +225,9 @@ int hstu_cache_append(const hstu_paged_cache* cache, const hstu_rotary_desc* rot
   if (q && ((rc = check_rows(q, size)) != HSTU_OK)) return rc;
   if (q && q->head_dim != cache->d_qk) return HSTU_ERR_BAD_SHAPE;
   if (cache->batch == 0 || new_rows == 0) return HSTU_OK;
-  if (!k || !v || !seq_offsets || (cache->ts_pages != nullptr) != (timestamps != nullptr)) return HSTU_ERR_NULL_PTR;
+  if (!k || !v || !seq_offsets) return HSTU_ERR_NULL_PTR;
+  // (a cache without pages has no address for timestamps either, and no place for any)
+  if (cache->num_pages > 0 && (cache->ts_pages != nullptr) != (timestamps != nullptr)) return HSTU_ERR_NULL_PTR;
   if (!aligned16(k) || !aligned16(v)) return HSTU_ERR_MISALIGNED;
   if ((rc = check_cache_pointers(cache)) != HSTU_OK) return rc;
   if (q && (rc = check_row_pointers(q)) != HSTU_OK) return rc;

@@ -65,3 +65,22 @@ def test_offsets_beyond_the_rows():
     assert torch.equal(qs[0], qs[1]) and torch.equal(cache.k_pages, other.k_pages) and torch.equal(cache.v_pages, other.v_pages)
     outs = [hstu.hstu_paged_attn_fwd(qs[0], c, o, 40, 0.2) for c, o in ((cache, off), (other, far))]
     assert torch.equal(outs[0], outs[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_cache_with_timestamps_and_without_pages(dtype):
+    """Rows have no places: queries are turned, keys and timestamps are dropped, and the attention with the bias gives zeros."""
+    none = torch.empty((0, 2, 16, 64), dtype=DT[dtype], device="cuda")
+    table = torch.zeros((3, 40), dtype=torch.int32, device="cuda")
+    lens, off = torch.tensor([20, 500, 9], dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 101, 102], dtype=torch.int32, device="cuda")
+    cache = hstu.HstuPagedCache(none, none.clone(), table, lens, torch.empty((0, 16), dtype=torch.int32, device="cuda"))
+    x = torch.ones((102, 2, 64), dtype=DT[dtype], device="cuda")
+    ts = torch.arange(102, dtype=torch.int32, device="cuda")
+    freq = hstu.hstu_rotary_frequencies(64)
+    q = hstu.hstu_cache_append(cache, x, x, off, q=x, inv_freq=freq, timestamps=ts)
+    pos = torch.cat((torch.tensor([19]), torch.arange(400, 500), torch.tensor([8]))).to(torch.int32).cuda()
+    assert torch.equal(q, hstu.hstu_rotary_fwd([x], freq, positions=pos)[0])
+    w = torch.randn(16, device="cuda")
+    for causal in (True, False):
+        assert (hstu.hstu_paged_attn_bias_fwd(q, cache, off, ts, w, 2, 500, 0.1, causal) == 0).all()
+        assert (hstu.hstu_paged_attn_bias_fwd(q, cache, off, ts, w, 2, 500, 0.1, causal, max_kv=500) == 0).all()
