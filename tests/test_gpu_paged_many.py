@@ -104,3 +104,46 @@ def test_offsets_that_do_not_ascend(batch):
         hstu.hstu_paged_attn_fwd(q, wrong, off, 300, 0.1, causal, out=buf[64:64 + rows])
     assert (buf[:64] == 7).all() and (buf[64 + rows:] == 7).all()
     pr.check(_many(pr, cache))
+
+
+@pytest.mark.parametrize("batch", [5, 140])
+def test_captured(batch):
+    """Captured once and replayed while lengths change, the sums over the batch worked out by every workgroup or once, with eager work and
+    another workspace's calls in between."""
+    lens, new = [1301, 300, 64, 700, 40] + [30] * (batch - 5), [150, 41, 64, 12, 40] + [11] * (batch - 5)
+    pr = Problem("bf16", lens, new, HEADS, KV_HEADS, 64, 64, 16, seed=batch, fill=0.0)
+    pr.table = np.pad(pr.table, ((0, 0), (0, 200)), constant_values=-1)
+    pr.width = pr.table.shape[1]
+    cache, off, q = pr.cache(), torch.from_numpy(pr.off).cuda(), pr.q.cuda()
+    need = hstu.hstu_paged_attn_workspace_bytes(cache, HEADS, pr.rows)
+    assert need >= 2 * 512 * 128 * 64 * 4
+    ws, out = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    hstu.hstu_paged_attn_fwd(q, cache, off, pr.max_len, pr.alpha)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        hstu.hstu_paged_attn_fwd(q, cache, off, pr.max_len, pr.alpha, out=out, workspace=ws)
+    for i in range(4):
+        now = torch.tensor([max(n - 37 * i, 0) for n in lens], dtype=torch.int32)
+        cache.seq_lens.copy_(now)
+        q.normal_()
+        out.fill_(NAN)
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(hstu.hstu_paged_attn_fwd(q, cache, off, pr.max_len, pr.alpha), got)
+        ws.fill_(0xff)
+        pr.lens, pr.q = [int(n) for n in now], q.cpu()
+        pr.check(got)
+
+
+def test_two_streams_at_once():
+    prs = [_problem(64, 64, 16, True, seed=s) for s in (1, 2)]
+    caches, qs = [p.cache() for p in prs], [p.q.cuda() for p in prs]
+    off = torch.from_numpy(prs[0].off).cuda()
+    want = [hstu.hstu_paged_attn_fwd(q, c, off, p.max_len, p.alpha) for q, c, p in zip(qs, caches, prs)]
+    streams = [torch.cuda.Stream() for _ in prs]
+    torch.cuda.synchronize()
+    got = [[hstu.hstu_paged_attn_fwd(qs[i], caches[i], off, prs[i].max_len, prs[i].alpha, stream=s) for i, s in enumerate(streams)]
+           for _ in range(5)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(w, g) for pair in got for w, g in zip(want, pair))
