@@ -456,8 +456,10 @@ typedef struct {
  * append first.  A row that sees nothing gets zeros; rows of o outside every sequence are left alone.  bias: NULL, or the timestamp bias with the
  * timestamps of the new rows (those of the cached rows are the cache's; d_ts_weights is not used).  The work is divided
  * by the lengths on the device, long histories among many workgroups, whose partial sums are added in the order of the keys: results
- * repeat bit for bit, and depend on the batch only in the order of fp32 additions.  bf16: as in hstu_jagged_attn_fwd; a call
- * of few rows per sequence keeps P in two bf16 terms. */
+ * repeat bit for bit.  What else is in the batch changes the order of a row's fp32 additions and, in bf16, how its P is rounded: calls of
+ * more than 8 (new row, query head) pairs per sequence and key/value head, on average, round P to bf16 once, as hstu_jagged_attn_fwd
+ * does (off by 2.3e-3 of the norm); calls of fewer, and of short histories of any number, keep it in two bf16 terms (1.7e-3, the output's own
+ * rounding).  Infinities and NaN reach the rows that see them, as the formula says. */
 int hstu_paged_attn_fwd(const hstu_paged_attn_params* params, const hstu_paged_cache* cache, const hstu_ts_bias* bias,
                         const void* q, int64_t q_stride, const int32_t* seq_offsets, void* o, void* workspace,
                         size_t workspace_bytes, void* hip_stream);

@@ -1210,7 +1210,8 @@ def hstu_paged_attn_fwd(q: torch.Tensor, cache: HstuPagedCache, seq_offsets: tor
     causal: the new rows are the last seq_offsets[b + 1] - seq_offsets[b] rows of the cache (append them first) and see the rows up to
     their own; otherwise every row sees all cached rows of its sequence (candidates scored against a history).
     heads may be a multiple of the cache's.  max_kv: a bound on cache.seq_lens that the caller knows (a hint for the
-    division of the work; nothing is left out beyond it).
+    division of the work; nothing is left out beyond it).  Results repeat bit for bit for the same batch; in bf16, batches of more
+    than 8 pairs (row, query head sharing a key/value head) per sequence on average round P to bf16 once, others keep two terms of it.
     """
     return _paged_call("hstu_paged_attn_fwd", q, cache, seq_offsets, None, None, 0, max_len, alpha, causal, max_kv, out,
                        workspace, stream, out_dtype)

@@ -6,8 +6,8 @@
 // One new row reads every cached key and value of its sequence once and does 4 d flops per row of 4 d bytes (bf16): the pass is
 // bound by reading the cache, and everything here serves to keep loads in flight.
 //   - A wave is a worker of its own (no LDS, no barrier): it takes a run of the line of all work (hstu_paged.h) and streams
-//     blocks of keys through registers, the next block's loads issued before the present one is used; with two waves
-//     per SIMD that is up to 256 KB in flight per CU, four times what the memory's latency needs.
+//     blocks of keys through registers, the next block's loads issued before the present one is used: at d = 128 a
+//     block of 16 KB per wave, 64 KB in flight per CU with a worker per SIMD.
 //   - 16 (new row, query head) pairs that share a key/value head are one operand of the 16x16 matrix instructions: query heads
 //     that share keys, and a few new rows, cost no further reads.  One pair alone leaves 15 columns unused: the matrix pipe
 //     then still has 5 times the throughput that the loads can feed.
